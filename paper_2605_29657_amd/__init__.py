@@ -5,4 +5,4 @@ The compute path is ``liboccam.so`` (hand-written HIP kernels behind the C ABI o
 Importing this package loads nothing; the binding loads the library on first use
 and raises if it is missing.
 """
-__all__ = ["occam", "synth", "workloads"]
+__all__ = ["cache", "occam", "synth", "workloads"]

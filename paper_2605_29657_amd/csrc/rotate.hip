@@ -1,0 +1,132 @@
+// Rotary positions with several axes: pair p of every head of a row turns by
+// positions[row][axis[p]] * inv_freq[p].
+//
+// The angle.  A position's turns are kept as a 64-bit fraction, F_p = inv_freq_p / 2 pi in
+// units of 2^-64, so position * F_p modulo 2^64 is the angle's fraction of a turn with no
+// rounding but F's own: exact where a float32 product (error 2^-24 of the angle) would
+// be wrong by a radian at position 10^7.  Sine and cosine take the fraction in
+// half-turns, rounded once to float32 (an angle error of pi 2^-25).
+//
+// Bound by memory: every element is read and written once, and a row's sines and cosines
+// are computed once for all heads of all tensors (queries and keys share a launch), staged
+// in LDS.  A workgroup takes a run of rows; a thread's unit is VEC bytes of each side of
+// the pairs (two 16-byte loads and stores where alignment allows), heads and chunks
+// spread over the threads so that consecutive threads touch consecutive addresses.
+#include "cache_internal.hpp"
+
+namespace occam {
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotPairs = 2048;          // (row, pair) angles a workgroup holds
+
+template <typename T> __device__ __forceinline__ float to_f(T x);
+template <> __device__ __forceinline__ float to_f(unsigned short x) { return __uint_as_float((unsigned)x << 16); }
+template <> __device__ __forceinline__ float to_f(float x) { return x; }
+template <typename T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ float from_f(float x) { return x; }
+template <> __device__ __forceinline__ unsigned short from_f(float x) {
+    return __builtin_bit_cast(unsigned short, (__bf16)x);
+}
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack { T x[N]; };
+
+// N elements per unit (a power of two; both sides of N pairs for HALVES, N / 2 pairs for
+// ADJACENT when N > 1).
+template <typename T, int N, bool ADJ>
+__global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
+    __shared__ float2 cs[kRotPairs];
+    const int row0 = blockIdx.x * rows_per;
+    const int rows = a.rows - row0 < rows_per ? a.rows - row0 : rows_per;
+    for (int i = threadIdx.x; i < rows * a.pairs; i += kRotThreads) {
+        const int r = i / a.pairs, p = i - r * a.pairs;
+        const int pos = a.pos[(size_t)(row0 + r) * a.axes + a.axis[p]];
+        const long long turn = (long long)((unsigned long long)(long long)pos * a.turn[p]);
+        // Signed fraction of a turn in 2^-32, then half-turns in (-1, 1].
+        const float half = (float)(int)((turn + (1ll << 31)) >> 32) * 0x1p-31f;
+        float s, c;
+        sincospif(half, &s, &c);
+        cs[i] = make_float2(c, a.inverse ? -s : s);
+    }
+    __syncthreads();
+    typedef Pack<T, N> V;
+    // Units of a head: pairs first, then what is only copied (absent in place).
+    const int np = ADJ && N > 1 ? 2 * a.pairs / N : a.pairs / N;
+    const int rest = (a.d - 2 * a.pairs) / N, per = np + rest, total = rows * a.heads * per;
+    for (int u = threadIdx.x; u < total; u += kRotThreads) {
+        const int hr = u / per, w = u - hr * per;
+        const int r = hr / a.heads, hh = hr - r * a.heads;
+        int ti = 0;
+        while (ti + 1 < a.n && hh >= a.t[ti + 1].first) ++ti;
+        const RotTensor& t = a.t[ti];
+        const size_t col = (size_t)(hh - t.first) * a.d;
+        const T* x = reinterpret_cast<const T*>(t.src + (size_t)(row0 + r) * t.src_stride) + col;
+        T* y = reinterpret_cast<T*>(t.dst + (size_t)(row0 + r) * t.dst_stride) + col;
+        if (w >= np) {
+            if (x == y) continue;
+            const int e = 2 * a.pairs + (w - np) * N;
+            *reinterpret_cast<V*>(y + e) = *reinterpret_cast<const V*>(x + e);
+            continue;
+        }
+        const float2* f = cs + r * a.pairs;
+        if constexpr (ADJ && N == 1) {
+            const float2 q = f[w];
+            const float p0 = to_f<T>(x[2 * w]), p1 = to_f<T>(x[2 * w + 1]);
+            y[2 * w] = from_f<T>(p0 * q.x - p1 * q.y);
+            y[2 * w + 1] = from_f<T>(p0 * q.y + p1 * q.x);
+        } else if constexpr (ADJ) {
+            V v = *reinterpret_cast<const V*>(x + w * N);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float2 q = f[w * (N / 2) + i];
+                const float p0 = to_f<T>(v.x[2 * i]), p1 = to_f<T>(v.x[2 * i + 1]);
+                v.x[2 * i] = from_f<T>(p0 * q.x - p1 * q.y);
+                v.x[2 * i + 1] = from_f<T>(p0 * q.y + p1 * q.x);
+            }
+            *reinterpret_cast<V*>(y + w * N) = v;
+        } else {
+            V v0 = *reinterpret_cast<const V*>(x + w * N);
+            V v1 = *reinterpret_cast<const V*>(x + a.pairs + w * N);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float2 q = f[w * N + i];
+                const float p0 = to_f<T>(v0.x[i]), p1 = to_f<T>(v1.x[i]);
+                v0.x[i] = from_f<T>(p0 * q.x - p1 * q.y);
+                v1.x[i] = from_f<T>(p0 * q.y + p1 * q.x);
+            }
+            *reinterpret_cast<V*>(y + w * N) = v0;
+            *reinterpret_cast<V*>(y + a.pairs + w * N) = v1;
+        }
+    }
+}
+
+template <typename T, int N, bool ADJ>
+hipError_t go(const RotArgs& a, hipStream_t s) {
+    // Rows per workgroup: what the angle table holds, fewer while that leaves the chip empty.
+    int per = kRotPairs / a.pairs;
+    while (per > 1 && (a.rows + per - 1) / per < 2048) per >>= 1;
+    return launch(rotate<T, N, ADJ>, dim3((a.rows + per - 1) / per), dim3(kRotThreads), 0, s, a, per);
+}
+
+template <typename T, int N>
+hipError_t pick(const RotArgs& a, hipStream_t s) {
+    return a.adjacent ? go<T, N, true>(a, s) : go<T, N, false>(a, s);
+}
+
+}  // namespace
+
+// vec: elements per unit that every pointer, stride and the head layout allow.
+hipError_t launch_rotate(const RotArgs& a, int f32, int vec, hipStream_t s) {
+    if (f32) {
+        if (vec >= 4) return pick<float, 4>(a, s);
+        if (vec >= 2) return pick<float, 2>(a, s);
+        return pick<float, 1>(a, s);
+    }
+    if (vec >= 8) return pick<unsigned short, 8>(a, s);
+    if (vec >= 4) return pick<unsigned short, 4>(a, s);
+    if (vec >= 2) return pick<unsigned short, 2>(a, s);
+    return pick<unsigned short, 1>(a, s);
+}
+
+}  // namespace occam

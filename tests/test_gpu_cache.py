@@ -1,0 +1,629 @@
+"""The serving side on the GPU against the plain 64-bit model of cache_model.py."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_29657_amd import cache, occam
+
+import cache_model as M
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def i32(x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def prefix(xs):
+    return [0] + [int(x) for x in np.cumsum(xs)]
+
+
+def same(a, b):
+    a, b = np.asarray(a), np.asarray(b)
+    assert a.shape == b.shape and np.array_equal(a, b), np.abs(a - b).max()
+
+
+class Cache:
+    """The library's cache and the model of it, driven together."""
+
+    def __init__(self, slots, page, Hkv, d, num_pages=64, max_pages=32, seed=0, dtype=torch.bfloat16):
+        self.pages = cache.Pages(num_pages, page, slots, max_pages)
+        self.layer = cache.Layer(self.pages, Hkv, d)
+        # What a page holds before it is written may be anything, NaN codes among it.
+        self.layer.k.fill_(0x7f)
+        self.layer.v.fill_(0xff)
+        self.layer.k_scale.fill_(float("nan"))
+        self.layer.v_scale.fill_(float("nan"))
+        self.page, self.Hkv, self.d, self.dtype = page, Hkv, d, dtype
+        self.k = [M.Sequence(page, Hkv, d) for _ in range(slots)]
+        self.v = [M.Sequence(page, Hkv, d) for _ in range(slots)]
+        self.gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.plan = cache.plan(self.pages, slots)
+
+    def rows(self, n, size=1.0):
+        x = torch.randn(n, self.Hkv, self.d, generator=self.gen, device=DEV) * size
+        x[::5] *= 20.0
+        return x.to(self.dtype)
+
+    def batch(self, seqs, rows):
+        return cache.Batch(len(seqs), seq=i32(seqs), row_offsets=i32(prefix(rows)), max_rows=max(max(rows), 1))
+
+    def append(self, seqs, rows, k=None, v=None, size=1.0):
+        b = self.batch(seqs, rows)
+        k = self.rows(sum(rows), size) if k is None else k
+        v = self.rows(sum(rows), size) if v is None else v
+        cache.reserve(self.pages, b, self.plan)
+        cache.append(self.pages, self.layer, b, self.plan, k, v)
+        at = 0
+        for s, r in zip(seqs, rows):
+            self.k[s].append(M.f64(k[at:at + r]))
+            self.v[s].append(M.f64(v[at:at + r]))
+            at += r
+        return k, v
+
+    def fork(self, src, dst):
+        cache.fork(self.pages, i32(src), i32(dst), self.plan)
+        for a, b in zip(src, dst):
+            self.k[b], self.v[b] = self.k[a].copy(), self.v[a].copy()
+
+    def free(self, seqs):
+        cache.free(self.pages, i32(seqs))
+        for s in seqs:
+            self.k[s], self.v[s] = (M.Sequence(self.page, self.Hkv, self.d) for _ in range(2))
+
+    def keep(self, seqs, starts, spans, kept):
+        flat, offs = i32([v for x in kept for v in x] or [0]), i32(prefix([len(x) for x in kept]))
+        cache.keep(self.pages, i32(seqs), i32(starts), i32(spans), flat, offs, self.plan)
+        cache.move(self.pages, self.layer, self.plan, flat, offs)
+        for s, a, m, x in zip(seqs, starts, spans, kept):
+            self.k[s].keep(a, m, x)
+            self.v[s].keep(a, m, x)
+
+    def read(self, seqs, dtype=None):
+        rows = [len(self.k[s].x) for s in seqs]
+        k = torch.full((sum(rows) + 3, self.Hkv, self.d), -7.0, dtype=dtype or self.dtype, device=DEV)
+        v = torch.full_like(k, -7.0)
+        if sum(rows):
+            cache.read(self.pages, self.layer, self.batch(seqs, rows), k, v)
+        return M.f64(k), M.f64(v), prefix(rows)
+
+    def check(self):
+        """Everything held equals the model, and the page state is consistent."""
+        p = self.pages
+        assert p.status.item() == 0
+        seqs = list(range(p.num_seqs))
+        k, v, at = self.read(seqs)
+        for s in seqs:
+            same(k[at[s]:at[s + 1]], self.k[s].x)
+            same(v[at[s]:at[s + 1]], self.v[s].x)
+        assert (k[at[-1]:] == -7).all() and (v[at[-1]:] == -7).all()
+        length, table = p.length.tolist(), p.table.tolist()
+        assert length == [len(x.x) for x in self.k]
+        refs = np.zeros(p.num_pages, int)
+        for s in seqs:
+            held = table[s][:-(-length[s] // self.page)]
+            assert len(set(held)) == len(held)
+            for g in held:
+                refs[g] += 1
+        assert p.refs.tolist() == refs.tolist()
+        words = p.taken.tolist()
+        for g in range(p.num_pages):
+            assert bool(words[g // 32] >> (g % 32) & 1) == (refs[g] > 0)
+
+
+# ------------------------------------------------------------------------------- rotary
+def rotary_case(d, pairs, axes, adjacent, dtype, rows, heads, far=0, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    pos = torch.randint(0, 5000, (rows, axes), generator=g, device=DEV, dtype=torch.int32) + far
+    freq = [1e6 ** (-p / pairs) for p in range(pairs)]
+    axis = [p % axes for p in range(pairs)]
+    xs = [torch.randn(rows, h, d, generator=g, device=DEV).to(dtype) for h in heads]
+    return cache.Rotary(d, freq, axis, axes, adjacent), pos, xs, axis, freq
+
+
+def check_rotated(got, x, pos, axis, freq, adjacent, inverse):
+    # Angle: pi 2^-25 (the fraction of a turn rounded to float32); sine and cosine within
+    # 2 ulp; two products and a sum; then half a step of the type.
+    want = M.turned(M.f64(x), pos.cpu().numpy().reshape(len(x), -1), axis, freq, adjacent, inverse)
+    n = len(freq)
+    size = np.abs(M.f64(x))
+    i = np.arange(n)
+    u, w = (2 * i, 2 * i + 1) if adjacent else (i, i + n)
+    mag = np.zeros_like(size)
+    mag[..., u] = mag[..., w] = size[..., u] + size[..., w]
+    tol = mag * (np.pi * 2.0 ** -25 + 2.0 ** -22 + 2.0 ** -23)
+    tol = tol + torch.finfo(x.dtype).eps / 2 * (np.abs(want) + tol)
+    assert np.all(np.abs(M.f64(got) - want) <= tol)
+    assert np.array_equal(M.f64(got)[..., 2 * n:], M.f64(x)[..., 2 * n:])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("d,pairs,axes", [(128, 64, 3), (72, 36, 2), (80, 20, 4), (6, 3, 1), (2, 1, 1),
+                                          (256, 128, 3), (64, 5, 2), (34, 8, 1)])
+def test_rotate(d, pairs, axes, adjacent, dtype):
+    for rows, heads, inverse, far in ((1, [3], False, 0), (77, [4, 1], True, -2500), (300, [2, 5, 1], False, 2 ** 30)):
+        r, pos, xs, axis, freq = rotary_case(d, pairs, axes, adjacent, dtype, rows, heads, far=far, seed=rows)
+        out = [torch.empty_like(x) for x in xs]
+        cache.rotate(r, pos, xs, out, inverse=inverse)
+        for o, x in zip(out, xs):
+            check_rotated(o, x, pos, axis, freq, adjacent, inverse)
+        copies = [x.clone() for x in xs]
+        cache.rotate(r, pos, copies, inverse=inverse)               # in place: the same bits
+        for o, c in zip(out, copies):
+            assert torch.equal(o, c)
+
+
+@pytest.mark.parametrize("off", [0, 1, 2, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rotate_views_of_one_projection(off, dtype):
+    # q and k as slices of a fused projection, at several alignments; the rest stays as it was.
+    H, Hkv, d, rows = 4, 2, 16, 37
+    r, pos, _, axis, freq = rotary_case(d, 8, 3, False, dtype, rows, [1])
+    base = torch.randn(rows, (H + 2 * Hkv) * d + 11, device=DEV).to(dtype)
+    was = base.clone()
+    q = base[:, off:off + H * d].unflatten(1, (H, d))
+    k = base[:, off + H * d:off + (H + Hkv) * d].unflatten(1, (Hkv, d))
+    cache.rotate(r, pos, [q, k])
+    end = off + (H + Hkv) * d
+    check_rotated(q, was[:, off:off + H * d].unflatten(1, (H, d)), pos, axis, freq, False, False)
+    check_rotated(k, was[:, off + H * d:end].unflatten(1, (Hkv, d)), pos, axis, freq, False, False)
+    assert torch.equal(base[:, :off], was[:, :off]) and torch.equal(base[:, end:], was[:, end:])
+
+
+def test_rotate_extreme_positions():
+    r, pos, xs, axis, freq = rotary_case(64, 32, 2, False, torch.float32, 4, [2])
+    pos.copy_(torch.tensor([[2 ** 31 - 1, -2 ** 31], [0, -1], [123456789, -987654321], [1, 2 ** 30]]))
+    out = [torch.empty_like(xs[0])]
+    cache.rotate(r, pos, xs, out)
+    check_rotated(out[0], xs[0], pos, axis, freq, False, False)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_inverse_is_the_gradient(adjacent):
+    # The rotation is linear: its gradient for an upstream w is the transpose applied to w,
+    # checked against the formula and against differences of <rotate(x), w>.
+    r, pos, (x, w), axis, freq = rotary_case(24, 10, 3, adjacent, torch.float32, 9, [3, 3])
+    grad, y = torch.empty_like(w), torch.empty_like(x)
+    cache.rotate(r, pos, [w], [grad], inverse=True)
+    check_rotated(grad, w, pos, axis, freq, adjacent, True)
+    cache.rotate(r, pos, [x], [y])
+    for e in (0, 7, 10, 21, 23):
+        step = x.clone()
+        step[4, 1, e] += 1.0
+        z = torch.empty_like(x)
+        cache.rotate(r, pos, [step], [z])
+        diff = ((z - y).double() * w.double()).sum().item()
+        # Each of the d elements of z - y is off by a few float32 roundings of |x| + 1.
+        room = 24 * 2.0 ** -21 * (x.abs().max().item() + 1) * w.abs().max().item()
+        assert abs(diff - grad[4, 1, e].item()) <= room
+
+
+# ------------------------------------------------------------------------- append and read
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page,Hkv,d", [(16, 1, 8), (16, 4, 80), (32, 2, 128), (64, 8, 128), (128, 2, 64),
+                                        (256, 1, 256), (64, 3, 256), (32, 5, 72)])
+def test_append_and_read(page, Hkv, d, dtype):
+    c = Cache(6, page, Hkv, d, num_pages=80, max_pages=40, dtype=dtype)
+    c.append([4, 0, 2, 5], [1, page - 1, page, 2 * page + 3])
+    c.check()
+    c.append([5, 0, 1, 4, 2], [1, 1, 0, page + 1, 1], size=1e-3)
+    c.append([0, 2, 4], [3, 1, 2], size=300.0)                      # scales grow, codes are rounded again
+    c.check()
+    k, v, at = c.read([5, 4], dtype=torch.float32)
+    same(k[:at[1]], c.k[5].x)
+    same(v[at[1]:at[2]], c.v[4].x)
+
+
+def test_one_token_at_a_time():
+    c = Cache(3, 16, 2, 64)
+    for step in range(37):
+        c.append([2, 0], [1, 1], size=10.0 ** (step % 7 - 3))
+    c.check()
+
+
+def test_extreme_magnitudes():
+    c = Cache(2, 16, 1, 8, dtype=torch.float32)
+    big = torch.zeros(5, 1, 8, device=DEV)
+    big[0], big[1], big[2, 0, :3] = 3.3e38, -3.3e38, torch.tensor([1e-38, 1e-30, 1.0], device=DEV)
+    tiny = torch.full((5, 1, 8), 2.0 ** -104, device=DEV)
+    c.append([0], [5], k=big, v=tiny)
+    c.append([0], [1], k=torch.zeros(1, 1, 8, device=DEV), v=torch.zeros(1, 1, 8, device=DEV))
+    c.append([1], [4], k=torch.zeros(4, 1, 8, device=DEV), v=torch.full((4, 1, 8), 1e-44, device=DEV))
+    c.check()
+
+
+def test_strided_rows_and_parts():
+    c = Cache(2, 32, 2, 64)
+    wide = torch.randn(50, 7 * 64, device=DEV).bfloat16()
+    k, v = wide[:, 64:192].unflatten(1, (2, 64)), wide[:, 256:384].unflatten(1, (2, 64))
+    c.append([1], [50], k=k, v=v)
+    c.check()
+    out = torch.full((40, 5, 64), 9.0, device=DEV).bfloat16()
+    # Tokens 13 .. of slot 1 and tokens -2 .. of slot 0 (which is empty), keys only, strided.
+    b = cache.Batch(2, rows=20, seq=i32([1, 0]))
+    cache.read(c.pages, c.layer, b, out[:, 1:3], None, start=i32([13, -2]))
+    same(M.f64(out[:20, 1:3]), c.k[1].x[13:33])
+    assert (out[20:] == 9).all() and (out[:, 0] == 9).all() and (out[:, 3:] == 9).all()
+    part = torch.full((20, 2, 64), 9.0, device=DEV).bfloat16()
+    cache.read(c.pages, c.layer, cache.Batch(1, rows=20, seq=i32([1])), None, part, start=i32([45]))
+    same(M.f64(part[:5]), c.v[1].x[45:])
+    assert (part[5:] == 9).all()
+    part.fill_(9.0)
+    cache.read(c.pages, c.layer, cache.Batch(1, rows=20, seq=i32([1])), None, part, start=i32([-3]))
+    same(M.f64(part[3:]), c.v[1].x[:17])
+    assert (part[:3] == 9).all()
+
+
+# ------------------------------------------------------------------------------- pages
+@pytest.mark.parametrize("page,d", [(16, 64), (64, 128)])
+def test_fork_and_copy_on_write(page, d):
+    c = Cache(6, page, 2, d)
+    c.append([0, 1], [page + 5, 2 * page])
+    c.fork([0, 0, 1], [2, 3, 4])
+    c.check()
+    c.append([0, 2, 3, 4], [1, 2, page, 1], size=50.0)             # every sharer moves off the shared tail
+    c.check()
+    c.fork([3], [5])
+    c.free([0, 3])
+    c.check()
+    c.append([5], [3])                                             # the last holder writes in place
+    c.check()
+    c.free([1, 2, 4, 5])
+    c.check()
+    assert c.pages.refs.sum().item() == 0
+
+
+def test_free_twice_in_one_call():
+    c = Cache(3, 16, 1, 64)
+    c.append([0, 1], [20, 40])
+    cache.free(c.pages, i32([1, 1, 2, 1]))
+    c.k[1], c.v[1] = M.Sequence(16, 1, 64), M.Sequence(16, 1, 64)
+    c.check()
+
+
+@pytest.mark.parametrize("page,Hkv,d", [(16, 2, 80), (64, 8, 128), (256, 1, 64), (32, 2, 256)])
+def test_keep(page, Hkv, d):
+    c = Cache(10, page, Hkv, d, num_pages=160)
+    lens = [3 * page + 7, 2 * page, page, 5, 4 * page + 1, 0]
+    c.append([0, 1, 2, 3, 4, 5], lens)
+    c.append([0, 4], [2, 3], size=100.0)
+    c.fork([0, 0, 4, 1], [6, 7, 8, 9])
+    rng = np.random.default_rng(page)
+
+    def some(n, share):
+        return sorted(rng.choice(n, int(n * share), replace=False).tolist())
+
+    c.keep([6, 1, 3, 8, 5, 7], [9, 0, 2, page + 3, 0, 4], [2 * page, 2 * page, 3, 2 * page, 0, 2 * page],
+           [some(2 * page, 0.3), [], [2], some(2 * page, 0.8), [], list(range(2 * page))])
+    c.check()
+    # A prefix of the span, then half of it.
+    c.keep([0, 9], [5, 0], [page, 2 * page], [list(range(page // 2)), some(2 * page, 0.5)])
+    c.check()
+    c.append([6, 1, 8, 9], [3, page + 1, 1, 2])
+    c.check()
+    c.keep([6, 1], [0, 0], [len(c.k[6].x), len(c.k[1].x)], [[], [0]])
+    c.check()
+    c.free(list(range(10)))
+    c.check()
+
+
+def state(c):
+    p = c.pages
+    return [t.clone() for t in (p.length, p.refs, p.taken, p.table, c.layer.k, c.layer.v,
+                                c.layer.k_scale.view(torch.int32))]
+
+
+def unchanged(c, was, bit):
+    torch.cuda.synchronize()
+    assert c.pages.status.item() == bit
+    for a, b in zip(was, state(c)):
+        assert torch.equal(a, b)
+    c.pages.status.zero_()
+
+
+def test_refused_on_the_device():
+    c = Cache(6, 16, 2, 64, num_pages=12, max_pages=6)
+    c.append([0, 1, 2], [90, 20, 33])                              # 6 + 2 + 3 pages: one is free
+    was = state(c)
+    k = c.rows(200)
+
+    def attempt(seqs, rows):
+        b = c.batch(seqs, rows)
+        cache.reserve(c.pages, b, c.plan)
+        cache.append(c.pages, c.layer, b, c.plan, k[:sum(rows)], k[:sum(rows)])
+
+    attempt([1, 3], [13, 1])                                       # two pages wanted
+    unchanged(c, was, cache.FULL)
+    attempt([1, 0], [1, 7])                                        # 97 tokens in a table of 96
+    unchanged(c, was, cache.TOO_LONG)
+    for seqs in ([1, 1], [1, 6], [-1, 1], [3, 70000]):
+        attempt(seqs, [1, 1])
+        unchanged(c, was, cache.BAD_SEQ)
+    for src, dst in (([0, 1], [3, 3]), ([0], [1]), ([0, 9], [3, 4]), ([0], [-1]), ([0], [6])):
+        cache.fork(c.pages, i32(src), i32(dst), c.plan)
+        unchanged(c, was, cache.BAD_SEQ)
+    cache.free(c.pages, i32([6, -3, 5]))
+    unchanged(c, was, cache.BAD_SEQ)
+    for seqs, start, span, n, bit in (([1], [5], [16], 3, cache.BAD_SPAN), ([1], [-1], [4], 2, cache.BAD_SPAN),
+                                      ([1], [0], [4], 5, cache.BAD_SPAN), ([1], [0], [-2], 0, cache.BAD_SPAN),
+                                      ([2, 2], [0, 0], [4, 4], 2, cache.BAD_SEQ), ([7], [0], [0], 0, cache.BAD_SEQ),
+                                      ([0], [0], [90], 40, cache.FULL)):
+        m = len(seqs)
+        idx, offs = i32(list(range(0, 2 * n * m, 2)) or [0]), i32([n * x for x in range(m + 1)])
+        cache.keep(c.pages, i32(seqs), i32(start), i32(span), idx, offs, c.plan)
+        cache.move(c.pages, c.layer, c.plan, idx, offs)
+        unchanged(c, was, bit)
+    # A plan of another kind writes nothing.
+    cache.append(c.pages, c.layer, c.batch([1], [1]), c.plan, k[:1], k[:1])
+    unchanged(c, was, 0)
+    c.append([1], [12])                                            # the last page is still there
+    c.check()
+
+
+def test_indices_outside_the_span_stay_inside_the_sequence():
+    c = Cache(2, 16, 1, 64)
+    c.append([0], [50])
+    idx, offs = i32([-5, 3, 1000000, 4]), i32([0, 4])
+    cache.keep(c.pages, i32([0]), i32([10]), i32([20]), idx, offs, c.plan)
+    cache.move(c.pages, c.layer, c.plan, idx, offs)
+    torch.cuda.synchronize()
+    assert c.pages.length.tolist() == [34, 0] and c.pages.status.item() == 0
+
+
+def test_many_sequences_and_a_large_pool():
+    # More sequences than a workgroup has threads, pages over many words of the map.
+    n, page = 2500, 16
+    pages = cache.Pages(70000, page, n, 40)
+    plan = cache.plan(pages, n)
+    rng = np.random.default_rng(5)
+    order, lens = rng.permutation(n), np.zeros(n, int)
+    for _ in range(2):
+        rows = rng.integers(0, 60, n)
+        cache.reserve(pages, cache.Batch(n, seq=i32(order), row_offsets=i32(prefix(rows)), max_rows=60), plan)
+        lens[order] += rows
+    assert pages.length.tolist() == lens.tolist() and pages.status.item() == 0
+    table = pages.table.cpu().numpy()
+    held = np.concatenate([table[s, :-(-l // page)] for s, l in enumerate(lens)])
+    assert sorted(held) == list(range(len(held)))                  # lowest pages first, each once
+    cache.free(pages, i32(range(0, n, 2)))
+    assert pages.refs.sum().item() == sum(-(-l // page) for l in lens[1::2])
+    bits = np.unpackbits(pages.taken.cpu().numpy().view(np.uint8), bitorder="little")
+    assert np.array_equal(bits[:70000], (pages.refs.cpu().numpy() > 0).astype(np.uint8))
+
+
+# --------------------------------------------------------------------------- attention
+def attend(c, seqs, rows, H, causal=True, scale=0.0, max_tokens=0, want_lse=True, q=None):
+    n = sum(rows)
+    q = torch.randn(n, H, c.d, generator=c.gen, device=DEV).bfloat16() if q is None else q
+    b = c.batch(seqs, rows)
+    ws = cache.workspace(c.pages, c.layer, b, H, max_tokens)
+    ws.fill_(0xff)
+    out = torch.full((n + 2, H, c.d), 5.0, device=DEV).bfloat16()
+    lse = torch.full((n + 2, H), 5.0, device=DEV)
+    cache.attend(c.pages, c.layer, b, q, out[:n], ws, lse=lse[:n] if want_lse else None, causal=causal,
+                 softmax_scale=scale, max_tokens=max_tokens)
+    assert (out[n:] == 5).all() and (lse[n:] == 5).all()
+    at = prefix(rows)
+    for i, s in enumerate(seqs):
+        x = slice(at[i], at[i + 1])
+        if rows[i]:
+            M.check_attention(M.f64(out[x]), M.f64(lse[x]) if want_lse else None, M.f64(q[x]), c.k[s].x, c.v[s].x,
+                              causal, scale)
+    return out[:n], lse[:n]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page,H,Hkv,d", [(16, 1, 1, 8), (16, 4, 2, 64), (64, 8, 2, 128), (32, 7, 1, 80),
+                                          (128, 16, 16, 128), (64, 6, 2, 256), (256, 40, 5, 96), (64, 32, 1, 64)])
+def test_attend(page, H, Hkv, d, causal):
+    c = Cache(8, page, Hkv, d, num_pages=400, max_pages=200, seed=page + d)
+    lens = [1, 2, 17, 64, 131, 330, 0, 700]
+    c.append(list(range(8)), lens)
+    # One row each; more rows than a block; rows without keys; sequences without rows.
+    attend(c, list(range(8)), [1] * 8, H, causal)
+    attend(c, [7, 2, 5, 3], [3, 17, 40, 0], H, causal)
+    attend(c, [5, 1, 6], [130, 7, 2], H, causal)
+    attend(c, [7, 4], [129, 131], H, causal, max_tokens=300)       # longer than the stated bound
+    attend(c, [3, 4], [1, 2], H, causal, scale=0.7, want_lse=False)
+    c.check()
+
+
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 33, 64, 100, 257])
+def test_attend_uniform_rows_and_strides(T):
+    c = Cache(3, 64, 2, 128, num_pages=100, max_pages=40)
+    c.append([0, 1, 2], [300, 257, 411])
+    H = 8
+    wide = torch.randn(3 * T, H + 3, 128, generator=c.gen, device=DEV).bfloat16()
+    out = torch.full((3 * T, H + 1, 128), 3.0, device=DEV).bfloat16()
+    lse = torch.empty(3 * T, H, device=DEV)
+    b = cache.Batch(3, rows=T)
+    cache.attend(c.pages, c.layer, b, wide[:, 2:2 + H], out[:, :H], cache.workspace(c.pages, c.layer, b, H), lse=lse)
+    assert (out[:, H] == 3).all()
+    for s in range(3):
+        x = slice(s * T, s * T + T)
+        M.check_attention(M.f64(out[x, :H]), M.f64(lse[x]), M.f64(wide[x, 2:2 + H]), c.k[s].x, c.v[s].x, True)
+
+
+@pytest.mark.parametrize("T", [1, 70])
+def test_attend_pages_of_unequal_scale(T):
+    # Value pages from 1e-6 to 1e4, the large ones late (the running reference moves) or early.
+    for sizes in ([1e-6, 1.0, 1e-3, 1e4], [1e4, 1e-6, 1.0, 1e-3]):
+        c = Cache(1, 16, 1, 64)
+        for z in sizes:
+            c.append([0], [48], size=z, k=c.rows(48, 0.3))
+        attend(c, [0], [T], 4)
+
+
+@pytest.mark.parametrize("T", [1, 80])
+def test_attend_sharp_and_flat_rows(T):
+    # One key far above the rest, and queries of zero (every key the same weight).
+    c = Cache(1, 64, 1, 128)
+    k = c.rows(500, 0.05)
+    k[123] = 4.0
+    c.append([0], [500], k=k)
+    q = torch.zeros(T, 4, 128, device=DEV).bfloat16()
+    q[:, 1], q[:, 2], q[:, 3] = 1.0, -1.0, 3.0
+    attend(c, [0], [T], 4, q=q)
+
+
+@pytest.mark.parametrize("L", [5000, 9001])
+def test_attend_long(L):
+    c = Cache(2, 64, 1, 128, num_pages=400, max_pages=200)
+    c.append([0, 1], [L, 300])
+    attend(c, [0, 1], [1, 1], 4)
+    attend(c, [1, 0], [20, 35], 4)
+
+
+def test_attend_repeats_bitwise_and_on_another_stream():
+    c = Cache(4, 64, 2, 128, num_pages=200, max_pages=100)
+    c.append([0, 1, 2, 3], [1000, 77, 3000, 512])
+    for rows in ([1, 1, 1, 1], [64, 5, 300, 1]):
+        q = torch.randn(sum(rows), 8, 128, generator=c.gen, device=DEV).bfloat16()
+        want = attend(c, [0, 1, 2, 3], rows, 8, q=q)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got = attend(c, [0, 1, 2, 3], rows, 8, q=q)
+        torch.cuda.synchronize()
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_storage_past_4_gib():
+    # 600000 pages of 8 KB: a sequence behind 32-bit offsets, the pages before it held by
+    # another that was only reserved.
+    page, Hkv, d = 64, 1, 128
+    pages = cache.Pages(600000, page, 4, 600000)
+    layer = cache.Layer(pages, Hkv, d)
+    p = cache.plan(pages, 1)
+    cache.reserve(pages, cache.Batch(1, rows=599000 * page, seq=i32([3])), p)
+    k, v = (torch.randn(1500, Hkv, d, device=DEV).bfloat16() for _ in range(2))
+    b = cache.Batch(1, rows=1500, seq=i32([1]))
+    cache.reserve(pages, b, p)
+    cache.append(pages, layer, b, p, k, v)
+    assert pages.table[1, 0].item() == 599000 and pages.status.item() == 0
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    cache.read(pages, layer, b, ko, vo)
+    m = M.Sequence(page, Hkv, d), M.Sequence(page, Hkv, d)
+    m[0].append(M.f64(k)), m[1].append(M.f64(v))
+    same(M.f64(ko), m[0].x)
+    same(M.f64(vo), m[1].x)
+    for T in (1, 90):
+        q = torch.randn(T, 4, d, device=DEV).bfloat16()
+        out, lse = torch.empty_like(q), torch.empty(T, 4, device=DEV)
+        bt = cache.Batch(1, rows=T, seq=i32([1]))
+        cache.attend(pages, layer, bt, q, out, cache.workspace(pages, layer, bt, 4, 1500), lse=lse, max_tokens=1500)
+        M.check_attention(M.f64(out), M.f64(lse), M.f64(q), m[0].x, m[1].x, True)
+    kept = list(range(0, 1000, 3))
+    idx, offs = i32(kept), i32([0, len(kept)])
+    cache.keep(pages, i32([1]), i32([100]), i32([1000]), idx, offs, p)
+    cache.move(pages, layer, p, idx, offs)
+    m[0].keep(100, 1000, kept), m[1].keep(100, 1000, kept)
+    n = len(m[0].x)
+    cache.read(pages, layer, cache.Batch(1, rows=n, seq=i32([1])), ko, vo)
+    same(M.f64(ko[:n]), m[0].x)
+    same(M.f64(vo[:n]), m[1].x)
+
+
+# ---------------------------------------------------------------------------- together
+def serving_step(c, rot, pos, q, k, v, qr, kr, b, src, dst, ws, out, lse):
+    cache.fork(c.pages, src, dst, c.plan)
+    cache.rotate(rot, pos, [q, k], [qr, kr])
+    cache.reserve(c.pages, b, c.plan)
+    cache.append(c.pages, c.layer, b, c.plan, kr, v)
+    cache.attend(c.pages, c.layer, b, qr, out, ws, lse=lse)
+    cache.free(c.pages, dst)
+
+
+def test_two_captured_steps_replay_beside_eager_ones():
+    c = Cache(12, 64, 2, 128, num_pages=200, max_pages=60)
+    c.append([0, 1, 2, 3], [130, 64, 1000, 1])
+    H = 8
+    rot = cache.Rotary(128, [1e6 ** (-p / 64) for p in range(64)], cache.interleaved([24, 20, 20]), 3)
+    sides = []
+    for T, base in ((1, 4), (9, 8)):
+        b = cache.Batch(4, rows=T, seq=i32(range(base, base + 4)))
+        q = torch.randn(4 * T, H, 128, generator=c.gen, device=DEV).bfloat16()
+        k, v = c.rows(4 * T), c.rows(4 * T)
+        pos = torch.randint(0, 9000, (4 * T, 3), generator=c.gen, device=DEV, dtype=torch.int32)
+        ws = cache.workspace(c.pages, c.layer, b, H)
+        sides.append((c, rot, pos, q, k, v, torch.empty_like(q), torch.empty_like(k), b, i32(range(4)),
+                      i32(range(base, base + 4)), ws, torch.empty_like(q), torch.empty(4 * T, H, device=DEV)))
+    want = []
+    for s in sides:
+        serving_step(*s)
+        torch.cuda.synchronize()
+        want.append((s[-2].clone(), s[-1].clone()))
+    graphs = []
+    for s in sides:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            serving_step(*s)
+        graphs.append(g)
+    for rep in range(3):
+        for g, s, w in zip(graphs, sides, want):
+            s[-2].fill_(1), s[-1].fill_(1)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(s[-2], w[0]) and torch.equal(s[-1], w[1])
+            serving_step(*s)                                       # eager work between the replays
+        c.check()
+
+
+@pytest.mark.parametrize("page,H,Hkv", [(64, 8, 2), (16, 4, 4)])
+def test_prompt_pruned_by_its_text_rows(page, H, Hkv):
+    """A prompt [before ; registers ; visual ; text] goes through the cache, the text rows'
+    attention gives the normalisers, occam.prune chooses the survivors from the cached keys,
+    the cache drops the others, and the next token is decoded on what is left."""
+    B, R, d, before = 3, 4, 128, 6
+    N, T = [90, 200, 33], [20, 20, 20]
+    c = Cache(B, page, Hkv, d, num_pages=120, seed=page)
+    lens = [before + R + n + t for n, t in zip(N, T)]
+    axis, freq = cache.sections([16, 24, 24]), [1e6 ** (-p / 64) for p in range(64)]
+    rot = cache.Rotary(d, freq, axis, 3)
+    total, offs = sum(lens), prefix(lens)
+    q = torch.randn(total, H, d, generator=c.gen, device=DEV).bfloat16()
+    k, v = c.rows(total, 0.4), c.rows(total)
+    pos = torch.randint(0, 300, (total, 3), generator=c.gen, device=DEV, dtype=torch.int32)
+    qk = [q.clone(), k.clone()]
+    cache.rotate(rot, pos, qk)
+    check_rotated(qk[0], q, pos, axis, freq, False, False)
+    check_rotated(qk[1], k, pos, axis, freq, False, False)
+    q, k = qk
+    c.append(list(range(B)), lens, k=k, v=v)
+    # Text rows: the last T of every sequence; their normalisers cover the whole prompt.
+    tq = torch.cat([q[offs[b + 1] - T[b]:offs[b + 1]] for b in range(B)])
+    out, lse = attend(c, list(range(B)), T, H, q=tq)
+    # The keys Stage II scores, as the cache holds them: [registers ; visual].
+    keys = [R + n for n in N]
+    kd = torch.empty(sum(keys), Hkv, d, dtype=torch.bfloat16, device=DEV)
+    cache.read(c.pages, c.layer, c.batch(list(range(B)), keys), kd, None, start=i32([before] * B))
+    p = occam.Problem(B, H, Hkv, d, R, rows=T[0], key_offsets=i32(prefix(keys)), max_cands=max(N))
+    o = occam.prune_outputs(B, sum(N), sum(keys))
+    # The widest gap between neighbouring ratios near 30 % decides lambda.
+    ratio = []
+    for b in range(B):
+        kx = c.k[b].x[before:before + keys[b]]
+        s = np.einsum("thd,khd->htk", M.f64(tq[b * T[0]:(b + 1) * T[0]]), np.repeat(kx, H // Hkv, 1)) / np.sqrt(d)
+        a = np.exp(s - M.f64(lse[b * T[0]:(b + 1) * T[0]]).T[:, :, None]).mean(0)
+        ratio.append(a[:, R:].max(0) / a[:, :R].mean())
+    flat = np.sort(np.concatenate(ratio))[::-1]
+    m = int(0.3 * len(flat))
+    j = m - 10 + int(np.argmax(flat[m - 10:m + 10] / flat[m - 9:m + 11]))
+    lam = float(np.sqrt(flat[j] * flat[j + 1]))
+    occam.prune(p, tq, kd, lam, o["kept_idx"], o["kept_count"], o["kept_offsets"], occam.workspace(p),
+                scores=o["scores"], tau=o["tau"], row_lse=lse)
+    cache.keep(c.pages, i32(range(B)), i32([before + R] * B), i32(N), o["kept_idx"], o["kept_offsets"], c.plan)
+    cache.move(c.pages, c.layer, c.plan, o["kept_idx"], o["kept_offsets"])
+    for b in range(B):
+        want = np.flatnonzero(ratio[b] >= lam)
+        a, e = o["kept_offsets"][b].item(), o["kept_offsets"][b + 1].item()
+        assert o["kept_idx"][a:e].tolist() == want.tolist()
+        c.k[b].keep(before + R, N[b], want)
+        c.v[b].keep(before + R, N[b], want)
+    c.check()
+    c.append(list(range(B)), [1] * B)
+    attend(c, list(range(B)), [1] * B, H)
+    c.check()
