@@ -292,20 +292,325 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
     }
 }
 
+// ---------------------------------------------------------------------------------------
+// Many rows: 32 rows of one key head per wave, WAVES waves per workgroup, which share every
+// tile of 64 keys and values through LDS.  The tile is converted to 16 bits once, on its way
+// into LDS (a wave that converted its own operands would spend as long on that as on the
+// products).  The running maximum only moves the sums when some row's maximum passed the
+// one in use by more than 2^8: probabilities are held times 2^6, so they stay below 2^14.
+// ---------------------------------------------------------------------------------------
+constexpr int kTile = 64;
+constexpr float kManyLift = 6.f, kManySlack = 8.f;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float max_over_halves(float x) {            // lanes l and l ^ 32
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// A barrier that orders LDS only: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
+template <int DP> constexpr int many_lds() { return 2 * 2 * kTile * DP * 2; }
+
+template <int DP>
+__global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
+    constexpr int WAVES = many_waves<DP>(), THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+    constexpr int NK = DP / 16;              // 16-element steps of the score product
+    constexpr int ND = DP / 32;              // 32-element tiles of the output
+    constexpr int CH = DP / 8;               // 16-byte chunks of a key row in LDS
+    constexpr int UK = kTile * DP / 16 / THREADS;    // key units (16 codes) per thread
+    constexpr int UV = kTile * DP / 16 / THREADS;    // value units (2 elements x 8 tokens)
+    static_assert(UK * THREADS * 16 == kTile * DP, "tile units");
+    extern __shared__ __align__(16) unsigned char lds[];
+    // [buffer][keys | values]: keys [64][DP] bf16, 16-byte chunk c of row m in slot
+    // c ^ (m % 16) (16 rows' reads of one chunk fall on all banks); values
+    // [tile of 32][16 tokens][half][DP][8 tokens] f16, the 8 reduction slots of a lane.
+    constexpr int HALF = kTile * DP * 2;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+    const int n = lane & 31, half = lane >> 5;
+    // Workgroups go round the eight XCDs; give each XCD a run of tasks, so that the row
+    // blocks of a key head, which read the same keys, share an L2.  Later row blocks first:
+    // under a causal mask they are the long ones.
+    int w;
+    {
+        const int total = gridDim.x, per = total >> 3, rest = total & 7;
+        const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
+        w = x * per + (x < rest ? x : rest) + k;
+    }
+    const int blocks = (((a.b.off ? a.b.max_rows : a.b.rows) * a.g) + ROWS - 1) / ROWS;
+    const int rb = blocks - 1 - w % blocks; w /= blocks;
+    const int sp = w % a.splits; w /= a.splits;
+    const int h = w % a.c.Hkv, i = w / a.c.Hkv;
+    const int T = row_count(a.b, i), slot = slot_of(a.b, i);
+    const int r0 = rb * ROWS;
+    if (r0 >= T * a.g) return;
+    const bool known = slot >= 0 && slot < a.pg.num_seqs;
+    const int len = known ? a.pg.length[slot] : 0;
+    auto block_end = [&](int first, int rows) {              // keys that these rows see
+        if (first >= T * a.g) return 0;
+        if (!a.causal) return len;
+        const int t = (first + rows - 1) / a.g;
+        return len - T + (t < T - 1 ? t : T - 1) + 1;
+    };
+    const int end = block_end(r0, ROWS);
+    const int lo = sp * a.chunk;
+    int hi = sp == a.splits - 1 ? end : lo + a.chunk;
+    hi = hi < end ? hi : end;
+    if (sp > 0 && lo >= end) return;
+    const int mine = uniform(block_end(r0 + wave * 32, 32));
+    const int wave_hi = mine < hi ? mine : hi;
+    const int* table = a.pg.table + (size_t)(known ? slot : 0) * a.pg.max_pages;
+    const int row = r0 + wave * 32 + n, t = row / a.g, hh = h * a.g + row - t * a.g;
+    const bool live = t < T;
+    const int last = live ? (a.causal ? len - T + t : len - 1) : -1;
+
+    bf16x8 q[NK];
+    {
+        const long long qrow = (long long)row_begin(a.b, i) + t;
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+            const int e = c * 16 + half * 8;
+            u32x4 x = {0, 0, 0, 0};
+            if (live && e < a.c.d)
+                x = *reinterpret_cast<const u32x4*>(a.q + qrow * a.q_stride + (long long)hh * a.c.d + e);
+            q[c] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+    f32x16 acc[ND] = {};
+    float m = -INFINITY, l = 0.f;            // m: the maximum in use, in base 2
+    int ref = kMinExp;                       // of the tile in LDS; the same in every wave
+
+    const int groups = hi > 0 ? (hi + 15) >> 4 : 0;
+    // Page numbers and scales of 64 groups of 16 tokens, one per lane, and the next 64's.
+    struct Win { int page; float ks; int ve; } win, nxt;
+    auto win_page = [&](int base) {
+        const int x = base + lane;
+        return x < groups ? table[x >> (a.pg.shift - 4)] : 0;
+    };
+    auto win_scales = [&](int base, Win& v) {
+        v.ks = 1.f;
+        v.ve = kMinExp;                      // no group: no claim on the reference
+        if (base + lane < groups) {
+            const size_t at = (size_t)v.page * a.c.Hkv + h;
+            v.ks = a.c.ks[at];
+            v.ve = exp_of(a.c.vs[at]);
+        }
+    };
+    // A tile on its way from memory to LDS: codes, and what converts them.
+    u32x4 rk[UK];
+    u32x2 rv[UV][2];
+    float sk[UK];
+    int sv[UV], top4 = kMinExp;
+    auto load_tile = [&](int pos, const Win& v) {
+        const int g0 = (pos >> 4) & 63;
+        top4 = kMinExp;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = __builtin_amdgcn_readlane(v.ve, g0 + k);
+            top4 = e > top4 ? e : top4;
+        }
+        auto block_of = [&](int gsel, const unsigned char* store) {
+            int gr = (pos >> 4) + gsel;
+            gr = gr < groups ? gr : groups - 1;       // masked keys, zeroed values
+            const int pg = __builtin_amdgcn_readlane(v.page, gr & 63);
+            const int tok = (gr << 4) & ((1 << a.pg.shift) - 1);
+            return store + ((size_t)pg * a.c.Hkv + h) * a.c.block + (size_t)tok * DP;
+        };
+#pragma unroll
+        for (int u = 0; u < UK; ++u) {
+            const int unit = u * THREADS + threadIdx.x;          // (row, 16 codes)
+            const int gsel = uniform(unit / (DP / 16) >> 4);
+            sk[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v.ks), g0 + gsel));
+            rk[u] = *reinterpret_cast<const u32x4*>(block_of(gsel, a.c.k) + (unit - gsel * DP) * 16);
+        }
+#pragma unroll
+        for (int u = 0; u < UV; ++u) {
+            const int unit = u * THREADS + threadIdx.x;          // (16 tokens, half, 2 elements)
+            const int gsel = uniform(unit / DP), x = unit - gsel * DP;
+            const int hf = x / (DP / 2), e = (x - hf * (DP / 2)) * 2;
+            sv[u] = __builtin_amdgcn_readlane(v.ve, g0 + gsel);
+            const unsigned char* p = block_of(gsel, a.c.v) + ((size_t)hf * DP + e) * 4;
+            rv[u][0] = *reinterpret_cast<const u32x2*>(p);
+            rv[u][1] = *reinterpret_cast<const u32x2*>(p + 2 * DP * 4);
+        }
+    };
+    auto store_tile = [&](int pos, int buf, int to) {
+        unsigned char* kd = lds + buf * 2 * HALF;
+        unsigned char* vd = kd + HALF;
+#pragma unroll
+        for (int u = 0; u < UK; ++u) {
+            const int unit = u * THREADS + threadIdx.x;
+            const int mrow = unit / (DP / 16), c = (unit - mrow * (DP / 16)) * 2;
+            const int sw = mrow & (CH < 16 ? CH - 1 : 15);
+            *reinterpret_cast<bf16x8*>(kd + mrow * DP * 2 + (c ^ sw) * 16) = codes_bf16(rk[u][0], rk[u][1], sk[u]);
+            *reinterpret_cast<bf16x8*>(kd + mrow * DP * 2 + ((c + 1) ^ sw) * 16) = codes_bf16(rk[u][2], rk[u][3], sk[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < UV; ++u) {
+            const int unit = u * THREADS + threadIdx.x;
+            const int gsel = uniform(unit / DP), x = unit - gsel * DP, hf = x / (DP / 2);
+            // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
+            if (pos + kTile > len) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int left = len - (pos + gsel * 16 + (hf + 2 * k) * 4);
+                    const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                    rv[u][k][0] &= keep;
+                    rv[u][k][1] &= keep;
+                }
+            }
+            const float sc = exp_scale(sv[u] - to < -126 ? -126 : sv[u] - to);
+            f16x8* d = reinterpret_cast<f16x8*>(vd + unit * 32);
+            d[0] = codes_f16(rv[u][0][0], sc, rv[u][1][0], sc);
+            d[1] = codes_f16(rv[u][0][1], sc, rv[u][1][1], sc);
+        }
+    };
+    auto compute = [&](int pos, int buf, int refs) {
+        const unsigned char* kd = lds + buf * 2 * HALF;
+        const unsigned char* vd = kd + HALF;
+        f32x16 s[2];
+        const int sw = n & (CH < 16 ? CH - 1 : 15);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NK; ++c)
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    *reinterpret_cast<const bf16x8*>(kd + (u * 32 + n) * DP * 2 + ((c * 2 + half) ^ sw) * 16),
+                    q[c], s[u], 0, 0, 0);
+        }
+        // The first of the wave's rows sees up to 31 keys fewer than the last.
+        if (pos + kTile > wave_hi || (a.causal && pos + kTile > mine - 32)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = pos + u * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
+                    s[u][e] = key <= last && key < hi ? s[u][e] : -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[0][e]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[1][e]);
+        top = max_over_halves(top) * a.scale2;
+        if (__any(top > m + kManySlack) || refs != ref) {
+            const float now = fmaxf(m, top);
+            const float fade = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+            const float fo = fade * exp_scale(ref - refs < -126 ? -126 : ref - refs);
+            l *= fade;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[d][e] *= fo;
+            m = now;
+            ref = refs;
+        }
+        const float base = m == -INFINITY ? 0.f : m - kManyLift;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f16x8 p[2];
+            float sum[2] = {0.f, 0.f};           // of the unrounded ones: the normaliser is float32
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float y0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale2, -base));
+                const float y1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale2, -base));
+                sum[0] += y0;
+                sum[1] += y1;
+                const f16x2 y = round_f16(y0, y1);
+                p[e >> 3][e & 7] = y[0];
+                p[e >> 3][(e & 7) + 1] = y[1];
+            }
+            l += sum[0] + sum[1];
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        *reinterpret_cast<const f16x8*>(vd + (((u * 2 + kk) * 2 + half) * DP + d * 32 + n) * 16),
+                        p[kk], acc[d], 0, 0, 0);
+        }
+    };
+    if (hi > lo) {
+        int base = (lo >> 4) & ~63;
+        win.page = win_page(base);
+        win_scales(base, win);
+        nxt = win;
+        load_tile(lo, win);
+        int to = top4;
+        store_tile(lo, 0, to);
+        lds_barrier();
+        int buf = 0;
+        for (int pos = lo; pos < hi; pos += kTile, buf ^= 1) {
+            const int in = (pos >> 4) & 63;           // 0, 4, ..: the tile's place in the window
+            if (in == 0 || pos == lo) nxt.page = win_page(base + 64);
+            if (in == 32 || (pos == lo && in > 32)) win_scales(base + 64, nxt);
+            if (in == 60) { win = nxt; base += 64; }
+            if (pos + kTile < hi) load_tile(pos + kTile, win);
+            if (pos < wave_hi) compute(pos, buf, to);
+            if (pos + kTile < hi) {
+                to = top4 > to ? top4 : to;
+                store_tile(pos + kTile, buf ^ 1, to);
+            }
+            lds_barrier();
+        }
+    }
+    l += __shfl_xor(l, 32);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) - kManyLift : -INFINITY;
+    if (!live) return;
+    const float f = exp_scale(ref);
+    const long long orow = (long long)row_begin(a.b, i) + t;
+    const size_t at = ((size_t)orow * a.H + hh) * a.splits + sp;
+    unsigned short* out = a.out + orow * a.out_stride + (long long)hh * a.c.d;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+            const int e0 = d * 32 + 8 * e4 + 4 * half;
+            if (e0 >= a.c.d) continue;
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = acc[d][e4 * 4 + e] * inv * f;
+            if (a.splits == 1) {
+                union { bf16x2 p[2]; u32x2 v; } o;
+                o.p[0] = bf16x2{(__bf16)y[0], (__bf16)y[1]};
+                o.p[1] = bf16x2{(__bf16)y[2], (__bf16)y[3]};
+                *reinterpret_cast<u32x2*>(out + e0) = o.v;
+            } else {
+                *reinterpret_cast<f32x4*>(a.part_o + at * a.c.d + e0) = f32x4{y[0], y[1], y[2], y[3]};
+            }
+        }
+    if (half == 0) {
+        if (a.splits == 1) { if (a.lse) a.lse[orow * a.H + hh] = lse2 * kLn2; }
+        else a.part_l[at] = lse2;
+    }
+}
+
 // Joins the splits of a row and head: weights 2^(lse - max), each split's output already
-// divided by its own sum.  A wave per (row, head).
-__global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
+// divided by its own sum.  A workgroup per (row, head): the splits are dealt to 1024 / DP
+// groups of threads, four elements a thread, so that a lone request's many splits are read
+// side by side.
+template <int DP>
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows) {
+    constexpr int TE = DP / 4, NG = 256 / TE;
+    __shared__ f32x4 jo[NG][TE];
+    __shared__ float js[NG];
     const int lane = threadIdx.x & 63;
-    const int maxr = a.b.off ? a.b.max_rows : a.b.rows;
-    const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int per = maxr * a.H;
-    const int i = (int)(w / per), x = (int)(w - (long long)i * per), t = x / a.H, hh = x - t * a.H;
-    if (i >= a.b.n) return;
+    const int maxr = a.b.off ? a.b.max_rows : a.b.rows, per = maxr * a.H;
+    const int i = blockIdx.x / per, x = blockIdx.x - i * per, t = x / a.H, hh = x - t * a.H;
     const int T = row_count(a.b, i), slot = slot_of(a.b, i);
     if (t >= T) return;
     const int len = slot >= 0 && slot < a.pg.num_seqs ? a.pg.length[slot] : 0;
     // The keys of the row block that the row was computed in decide which splits exist.
-    const int r = t * a.g + hh % a.g, r1 = (r / kFewRows + 1) * kFewRows - 1;
+    const int r = t * a.g + hh % a.g, r1 = (r / block_rows + 1) * block_rows - 1;
     const int tm = r1 / a.g < T - 1 ? r1 / a.g : T - 1;
     const int end = a.causal ? len - T + tm + 1 : len;
     int parts = end > 0 ? (end + a.chunk - 1) / a.chunk : 1;
@@ -316,52 +621,87 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_l[at + p]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float sum = 0.f, y[4] = {};
     const float base = top == -INFINITY ? 0.f : top;
-    for (int p = 0; p < parts; ++p) {
+    const int te = threadIdx.x % TE, grp = threadIdx.x / TE;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    const bool in = te * 4 < a.c.d;
+#pragma unroll 4
+    for (int p = grp; p < parts; p += NG) {
         const float wgt = __builtin_amdgcn_exp2f(a.part_l[at + p] - base);
         sum += wgt;
-        for (int e = lane, k = 0; e < a.c.d; e += 64, ++k) y[k] += wgt * a.part_o[(at + p) * a.c.d + e];
+        if (in) y += wgt * *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    unsigned short* o = a.out + orow * a.out_stride + (long long)hh * a.c.d;
-    for (int e = lane, k = 0; e < a.c.d; e += 64, ++k)
-        o[e] = __builtin_bit_cast(unsigned short, (__bf16)(y[k] * inv));
-    if (lane == 0 && a.lse)
+    jo[grp][te] = y;
+    if (te == 0) js[grp] = sum;
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int g = 1; g < NG; ++g) { y += jo[g][te]; sum += js[g]; }
+    y *= sum > 0.f ? 1.f / sum : 0.f;
+    if (in) {
+        ushort4 o;
+        o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
+        o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
+        o.z = __builtin_bit_cast(unsigned short, (__bf16)y[2]);
+        o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
+        *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)hh * a.c.d + te * 4) = o;
+    }
+    if (te == 0 && a.lse)
         a.lse[orow * a.H + hh] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
 }  // namespace
 
+// Which form: more rows than two blocks of the few-row form go to the many-row form.
+int attend_block_rows(const CacheView& c, const BatchView& b, int H) {
+    const long long rows = (long long)(b.off ? b.max_rows : b.rows) * (H / c.Hkv);
+    return rows <= 2 * kFewRows ? kFewRows : c.dp == 128 ? 256 : 128;
+}
+
 // Keys per split and splits: enough workgroups to fill the chip several times over, at
-// least 128 keys (a step of every wave) each.
+// least 128 keys each.
 void attend_splits(const CacheView& c, const BatchView& b, int H, long long max_tokens, int* chunk,
                    int* splits) {
+    const int br = attend_block_rows(c, b, H);
     const long long rows = (long long)(b.off ? b.max_rows : b.rows) * (H / c.Hkv);
-    const long long tasks = (long long)b.n * c.Hkv * ((rows + kFewRows - 1) / kFewRows);
-    const long long least = kStep * kFewWaves;
-    long long want = 2048 / tasks;
+    const long long tasks = (long long)b.n * c.Hkv * ((rows + br - 1) / br);
+    const long long least = 128;
+    long long want = (br == kFewRows ? 2048 : 512) / tasks;
     const long long most = (max_tokens + least - 1) / least;
     want = want < 1 ? 1 : want > most ? most : want;
     want = want < 1 ? 1 : want;
     long long per = (max_tokens + want - 1) / want;
-    per = (per + kStep - 1) / kStep * kStep;
+    per = (per + kTile - 1) / kTile * kTile;
     per = per < least ? least : per;
     *chunk = (int)per;
     *splits = (int)((max_tokens + per - 1) / per);
     if (*splits < 1) *splits = 1;
 }
 
-hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {
-    const long long rows = (long long)(a.b.off ? a.b.max_rows : a.b.rows) * a.g;
-    const long long blocks = (rows + kFewRows - 1) / kFewRows;
-    const dim3 grid((unsigned)(blocks * a.splits * a.c.Hkv * a.b.n)), block(64 * kFewWaves);
-    hipError_t e = a.c.dp == 64    ? launch(attend_few<64>, grid, block, 0, s, a)
-                   : a.c.dp == 128 ? launch(attend_few<128>, grid, block, 0, s, a)
-                                   : launch(attend_few<256>, grid, block, 0, s, a);
+template <int DP>
+static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
+    const int br = attend_block_rows(a.c, a.b, a.H);
+    const long long maxr = a.b.off ? a.b.max_rows : a.b.rows;
+    const long long blocks = (maxr * a.g + br - 1) / br;
+    const dim3 grid((unsigned)(blocks * a.splits * a.c.Hkv * a.b.n));
+    hipError_t e;
+    if (br == kFewRows) {
+        e = launch(attend_few<DP>, grid, dim3(64 * kFewWaves), 0, s, a);
+    } else {
+        static_assert(32 * many_waves<DP>() == (DP == 128 ? 256 : 128), "rows of a block");
+        constexpr int bytes = many_lds<DP>();
+        static std::atomic<uint64_t> done{0};
+        e = bytes <= 65536 ? hipSuccess
+                           : allow_lds(reinterpret_cast<const void*>(attend_many<DP>), bytes, done);
+        if (e == hipSuccess) e = launch(attend_many<DP>, grid, dim3(64 * many_waves<DP>()), bytes, s, a);
+    }
     if (e != hipSuccess || a.splits == 1) return e;
-    const long long waves = (long long)a.b.n * (a.b.off ? a.b.max_rows : a.b.rows) * a.H;
-    return launch(attend_join, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
+    return launch(attend_join<DP>, dim3((unsigned)(a.b.n * maxr * a.H)), dim3(256), 0, s, a, br);
+}
+
+hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {
+    return a.c.dp == 64 ? attend_dp<64>(a, s) : a.c.dp == 128 ? attend_dp<128>(a, s) : attend_dp<256>(a, s);
 }
 
 }  // namespace occam
