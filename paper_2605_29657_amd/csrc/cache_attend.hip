@@ -298,6 +298,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
 // into LDS (a wave that converted its own operands would spend as long on that as on the
 // products).  The running maximum only moves the sums when some row's maximum passed the
 // one in use by more than 2^8: probabilities are held times 2^6, so they stay below 2^14.
+//
+// Work alternates between matrix phases (the scores of tile t, the output of tile t - 1) and
+// vector phases (the softmax of tile t, the conversion of a tile to come), a barrier after
+// each.  With eight waves, the second four run one phase behind, so that of the two waves
+// of a SIMD one feeds the matrix core while the other does vector work.  The tile written
+// in vector phase t is t + AHEAD: with phases A: M(t) = 2t, V(t) = 2t + 1 and B: one later,
+// keys t are read until phase 2t + 1 and values t until 2t + 3, and the last share of tile
+// t is written in B's V(t - 2) = 2t - 2; four buffers keep every write past the last read of
+// the tile before (2 (t - 4) + 3 < 2 (t - 2) + 1).  One group needs one tile ahead and two
+// buffers.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr float kManyLift = 6.f, kManySlack = 8.f;
@@ -315,11 +325,13 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
-template <int DP> constexpr int many_lds() { return 2 * 2 * kTile * DP * 2; }
+template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
+template <int DP> constexpr int many_lds() { return many_bufs<DP>() * 2 * kTile * DP * 2; }
 
 template <int DP>
 __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
     constexpr int WAVES = many_waves<DP>(), THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+    constexpr int AHEAD = WAVES / 4, BUFS = many_bufs<DP>();
     constexpr int NK = DP / 16;              // 16-element steps of the score product
     constexpr int ND = DP / 32;              // 32-element tiles of the output
     constexpr int CH = DP / 8;               // 16-byte chunks of a key row in LDS
@@ -333,17 +345,11 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     constexpr int HALF = kTile * DP * 2;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 31, half = lane >> 5;
-    // Workgroups go round the eight XCDs; give each XCD a run of tasks, so that the row
-    // blocks of a key head, which read the same keys, share an L2.  Later row blocks first:
-    // under a causal mask they are the long ones.
-    int w;
-    {
-        const int total = gridDim.x, per = total >> 3, rest = total & 7;
-        const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
-        w = x * per + (x < rest ? x : rest) + k;
-    }
+    // Later row blocks of every sequence first: under a causal mask they are the long ones.
     const int blocks = (((a.b.off ? a.b.max_rows : a.b.rows) * a.g) + ROWS - 1) / ROWS;
-    const int rb = blocks - 1 - w % blocks; w /= blocks;
+    const int tasks = a.splits * a.c.Hkv * a.b.n;
+    int w = blockIdx.x;
+    const int rb = blocks - 1 - w / tasks; w %= tasks;
     const int sp = w % a.splits; w /= a.splits;
     const int h = w % a.c.Hkv, i = w / a.c.Hkv;
     const int T = row_count(a.b, i), slot = slot_of(a.b, i);
@@ -383,7 +389,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     }
     f32x16 acc[ND] = {};
     float m = -INFINITY, l = 0.f;            // m: the maximum in use, in base 2
-    int ref = kMinExp;                       // of the tile in LDS; the same in every wave
+    int ref = kMinExp;                       // of the values summed; the same in every wave
 
     const int groups = hi > 0 ? (hi + 15) >> 4 : 0;
     // Page numbers and scales of 64 groups of 16 tokens, one per lane, and the next 64's.
@@ -470,21 +476,34 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
             d[1] = codes_f16(rv[u][0][1], sc, rv[u][1][1], sc);
         }
     };
-    auto compute = [&](int pos, int buf, int refs) {
+    f32x16 s[2];
+    f16x8 p[4];
+    const int sw = n & (CH < 16 ? CH - 1 : 15);
+    auto scores = [&](int buf) {
         const unsigned char* kd = lds + buf * 2 * HALF;
-        const unsigned char* vd = kd + HALF;
-        f32x16 s[2];
-        const int sw = n & (CH < 16 ? CH - 1 : 15);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
 #pragma unroll
-            for (int c = 0; c < NK; ++c)
+        for (int c = 0; c < NK; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
                 s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                     *reinterpret_cast<const bf16x8*>(kd + (u * 32 + n) * DP * 2 + ((c * 2 + half) ^ sw) * 16),
                     q[c], s[u], 0, 0, 0);
-        }
+    };
+    auto output = [&](int buf) {
+        const unsigned char* vd = lds + buf * 2 * HALF + HALF;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    *reinterpret_cast<const f16x8*>(vd + ((kk * 2 + half) * DP + d * 32 + n) * 16), p[kk],
+                    acc[d], 0, 0, 0);
+    };
+    auto softmax = [&](int pos, int refs) {
         // The first of the wave's rows sees up to 31 keys fewer than the last.
         if (pos + kTile > wave_hi || (a.causal && pos + kTile > mine - 32)) {
 #pragma unroll
@@ -514,53 +533,61 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
             ref = refs;
         }
         const float base = m == -INFINITY ? 0.f : m - kManyLift;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};     // of the unrounded ones: the normaliser is float32
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            f16x8 p[2];
-            float sum[2] = {0.f, 0.f};           // of the unrounded ones: the normaliser is float32
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
                 const float y0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale2, -base));
                 const float y1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale2, -base));
-                sum[0] += y0;
-                sum[1] += y1;
+                sum[u * 2] += y0;
+                sum[u * 2 + 1] += y1;
                 const f16x2 y = round_f16(y0, y1);
-                p[e >> 3][e & 7] = y[0];
-                p[e >> 3][(e & 7) + 1] = y[1];
+                p[u * 2 + (e >> 3)][e & 7] = y[0];
+                p[u * 2 + (e >> 3)][(e & 7) + 1] = y[1];
             }
-            l += sum[0] + sum[1];
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        *reinterpret_cast<const f16x8*>(vd + (((u * 2 + kk) * 2 + half) * DP + d * 32 + n) * 16),
-                        p[kk], acc[d], 0, 0, 0);
-        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
     if (hi > lo) {
+        const int tiles = (hi - lo + kTile - 1) / kTile;
         int base = (lo >> 4) & ~63;
         win.page = win_page(base);
         win_scales(base, win);
         nxt = win;
-        load_tile(lo, win);
-        int to = top4;
-        store_tile(lo, 0, to);
+        auto fetch = [&](int tile) {
+            const int pos = lo + tile * kTile, in = (pos >> 4) & 63;
+            if (((pos >> 4) & ~63) != base) { win = nxt; base += 64; }
+            load_tile(pos, win);
+            if (in == 0 || tile == 0) nxt.page = win_page(base + 64);
+            if (in == 32 || (tile == 0 && in > 32)) win_scales(base + 64, nxt);
+        };
+        int refs[AHEAD + 1];                     // of tiles t .. t + AHEAD
+        int to = kMinExp;
+        auto keep = [&](int tile) {
+            to = top4 > to ? top4 : to;
+            store_tile(lo + tile * kTile, tile % BUFS, to);
+        };
+        for (int x = 0; x < AHEAD; ++x) {
+            if (x < tiles) { fetch(x); keep(x); }
+            refs[x] = to;
+        }
         lds_barrier();
-        int buf = 0;
-        for (int pos = lo; pos < hi; pos += kTile, buf ^= 1) {
-            const int in = (pos >> 4) & 63;           // 0, 4, ..: the tile's place in the window
-            if (in == 0 || pos == lo) nxt.page = win_page(base + 64);
-            if (in == 32 || (pos == lo && in > 32)) win_scales(base + 64, nxt);
-            if (in == 60) { win = nxt; base += 64; }
-            if (pos + kTile < hi) load_tile(pos + kTile, win);
-            if (pos < wave_hi) compute(pos, buf, to);
-            if (pos + kTile < hi) {
-                to = top4 > to ? top4 : to;
-                store_tile(pos + kTile, buf ^ 1, to);
-            }
+        const bool behind = AHEAD == 2 && wave >= 4;
+        if (behind) lds_barrier();
+        for (int tile = 0; tile <= tiles; ++tile) {
+            const int pos = lo + tile * kTile;
+            if (tile + AHEAD < tiles) fetch(tile + AHEAD);
+            if (tile > 0 && pos - kTile < wave_hi) output((tile - 1) % BUFS);
+            if (tile < tiles && pos < wave_hi) scores(tile % BUFS);
+            lds_barrier();
+            if (tile < tiles && pos < wave_hi) softmax(pos, refs[0]);
+            if (tile + AHEAD < tiles) keep(tile + AHEAD);
+#pragma unroll
+            for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
+            refs[AHEAD - 1] = to;
             lds_barrier();
         }
+        if (AHEAD == 2 && !behind) lds_barrier();
     }
     l += __shfl_xor(l, 32);
     const float inv = l > 0.f ? 1.f / l : 0.f;
