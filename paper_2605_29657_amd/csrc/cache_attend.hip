@@ -324,6 +324,20 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Orders a matrix phase of N products: operands are read from LDS kReads products ahead
+// (the compiler by itself reads two and waits for them).
+constexpr int kReads = 8;
+template <int N>
+__device__ __forceinline__ void operands_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+    for (int i = 0; i < N - kReads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, kReads, 0);
+}
+
 template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
 template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
 template <int DP> constexpr int many_lds() { return many_bufs<DP>() * 2 * kTile * DP * 2; }
@@ -571,20 +585,27 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
             if (x < tiles) { fetch(x); keep(x); }
             refs[x] = to;
         }
+        if (AHEAD < tiles) fetch(AHEAD);         // in flight until the next vector phase
         lds_barrier();
         const bool behind = AHEAD == 2 && wave >= 4;
         if (behind) lds_barrier();
-        for (int tile = 0; tile <= tiles; ++tile) {
+        scores(0);
+        lds_barrier();
+        for (int tile = 0; tile < tiles; ++tile) {
             const int pos = lo + tile * kTile;
-            if (tile + AHEAD < tiles) fetch(tile + AHEAD);
-            if (tile > 0 && pos - kTile < wave_hi) output((tile - 1) % BUFS);
-            if (tile < tiles && pos < wave_hi) scores(tile % BUFS);
-            lds_barrier();
-            if (tile < tiles && pos < wave_hi) softmax(pos, refs[0]);
+            if (pos < wave_hi) softmax(pos, refs[0]);
             if (tile + AHEAD < tiles) keep(tile + AHEAD);
+            if (tile + AHEAD + 1 < tiles) fetch(tile + AHEAD + 1);
 #pragma unroll
             for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
             refs[AHEAD - 1] = to;
+            lds_barrier();
+            if (pos < wave_hi) {
+                // (After the last tile the scores are of a stale one and unused.)
+                output(tile % BUFS);
+                scores((tile + 1) % BUFS);
+                operands_ahead<2 * NK + 4 * ND>();
+            }
             lds_barrier();
         }
         if (AHEAD == 2 && !behind) lds_barrier();
