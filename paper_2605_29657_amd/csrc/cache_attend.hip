@@ -406,8 +406,9 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     int ref = kMinExp;                       // of the values summed; the same in every wave
 
     const int groups = hi > 0 ? (hi + 15) >> 4 : 0;
-    // Page numbers and scales of 64 groups of 16 tokens, one per lane, and the next 64's.
-    struct Win { int page; float ks; int ve; } win, nxt;
+    // 64 groups of 16 tokens, one per lane, and the next 64: where a group's codes lie, its
+    // scales, and the largest value exponent of the four groups of its tile.
+    struct Win { int page; unsigned lo, hi; float ks; int ve, top; } win, nxt;
     auto win_page = [&](int base) {
         const int x = base + lane;
         return x < groups ? table[x >> (a.pg.shift - 4)] : 0;
@@ -415,79 +416,81 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     auto win_scales = [&](int base, Win& v) {
         v.ks = 1.f;
         v.ve = kMinExp;                      // no group: no claim on the reference
+        const size_t at = (size_t)v.page * a.c.Hkv + h;
+        size_t off = at * a.c.block;         // past the end: page 0, whose codes are masked
         if (base + lane < groups) {
-            const size_t at = (size_t)v.page * a.c.Hkv + h;
             v.ks = a.c.ks[at];
             v.ve = exp_of(a.c.vs[at]);
+            off += (size_t)(((base + lane) << 4) & ((1 << a.pg.shift) - 1)) * DP;
         }
+        v.lo = (unsigned)off;
+        v.hi = (unsigned)(off >> 32);
+        int o = __builtin_amdgcn_mov_dpp(v.ve, 0xB1, 15, 15, true);      // lane ^ 1
+        v.top = v.ve > o ? v.ve : o;
+        o = __builtin_amdgcn_mov_dpp(v.top, 0x4E, 15, 15, true);         // lane ^ 2
+        v.top = v.top > o ? v.top : o;
     };
-    // A tile on its way from memory to LDS: codes, and what converts them.
+    // A tile on its way from memory to LDS: codes, and what converts them.  Unit x of a
+    // group of 16 tokens: 16 codes of a key row; two elements of 8 tokens' values.
     u32x4 rk[UK];
     u32x2 rv[UV][2];
     float sk[UK];
     int sv[UV], top4 = kMinExp;
+    const int x0 = threadIdx.x % DP, hf = x0 / (DP / 2);
+    const unsigned koff = x0 * 16, voff = (hf * DP + (x0 - hf * (DP / 2)) * 2) * 4;
+    auto group_of = [&](int u) { return (u * THREADS + wave * 64) / DP; };
     auto load_tile = [&](int pos, const Win& v) {
         const int g0 = (pos >> 4) & 63;
-        top4 = kMinExp;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int e = __builtin_amdgcn_readlane(v.ve, g0 + k);
-            top4 = e > top4 ? e : top4;
-        }
-        auto block_of = [&](int gsel, const unsigned char* store) {
-            int gr = (pos >> 4) + gsel;
-            gr = gr < groups ? gr : groups - 1;       // masked keys, zeroed values
-            const int pg = __builtin_amdgcn_readlane(v.page, gr & 63);
-            const int tok = (gr << 4) & ((1 << a.pg.shift) - 1);
-            return store + ((size_t)pg * a.c.Hkv + h) * a.c.block + (size_t)tok * DP;
-        };
+        top4 = __builtin_amdgcn_readlane(v.top, g0);
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
-            const int unit = u * THREADS + threadIdx.x;          // (row, 16 codes)
-            const int gsel = uniform(unit / (DP / 16) >> 4);
-            sk[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v.ks), g0 + gsel));
-            rk[u] = *reinterpret_cast<const u32x4*>(block_of(gsel, a.c.k) + (unit - gsel * DP) * 16);
-        }
-#pragma unroll
-        for (int u = 0; u < UV; ++u) {
-            const int unit = u * THREADS + threadIdx.x;          // (16 tokens, half, 2 elements)
-            const int gsel = uniform(unit / DP), x = unit - gsel * DP;
-            const int hf = x / (DP / 2), e = (x - hf * (DP / 2)) * 2;
-            sv[u] = __builtin_amdgcn_readlane(v.ve, g0 + gsel);
-            const unsigned char* p = block_of(gsel, a.c.v) + ((size_t)hf * DP + e) * 4;
-            rv[u][0] = *reinterpret_cast<const u32x2*>(p);
-            rv[u][1] = *reinterpret_cast<const u32x2*>(p + 2 * DP * 4);
+            const int g = g0 + group_of(u);
+            sk[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v.ks), g));
+            sv[u] = __builtin_amdgcn_readlane(v.ve, g);
+            const size_t off = (unsigned)__builtin_amdgcn_readlane((int)v.lo, g) |
+                               (size_t)(unsigned)__builtin_amdgcn_readlane((int)v.hi, g) << 32;
+            const unsigned char* kp = a.c.k + off;
+            const unsigned char* vp = a.c.v + off;
+            rk[u] = *reinterpret_cast<const u32x4*>(kp + koff);
+            rv[u][0] = *reinterpret_cast<const u32x2*>(vp + voff);
+            rv[u][1] = *reinterpret_cast<const u32x2*>(vp + voff + 2 * DP * 4);
         }
     };
+    // Where this thread's units go, relative to the buffer.
+    unsigned kto[UK][2], vto[UV];
+#pragma unroll
+    for (int u = 0; u < UK; ++u) {
+        const int unit = u * THREADS + threadIdx.x;
+        const int mrow = unit / (DP / 16), c = (unit - mrow * (DP / 16)) * 2;
+        const int swz = mrow & (CH < 16 ? CH - 1 : 15);
+        kto[u][0] = mrow * DP * 2 + (c ^ swz) * 16;
+        kto[u][1] = mrow * DP * 2 + ((c + 1) ^ swz) * 16;
+        vto[u] = HALF + unit * 32;
+    }
     auto store_tile = [&](int pos, int buf, int to) {
-        unsigned char* kd = lds + buf * 2 * HALF;
-        unsigned char* vd = kd + HALF;
+        unsigned char* d = lds + buf * 2 * HALF;
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
-            const int unit = u * THREADS + threadIdx.x;
-            const int mrow = unit / (DP / 16), c = (unit - mrow * (DP / 16)) * 2;
-            const int sw = mrow & (CH < 16 ? CH - 1 : 15);
-            *reinterpret_cast<bf16x8*>(kd + mrow * DP * 2 + (c ^ sw) * 16) = codes_bf16(rk[u][0], rk[u][1], sk[u]);
-            *reinterpret_cast<bf16x8*>(kd + mrow * DP * 2 + ((c + 1) ^ sw) * 16) = codes_bf16(rk[u][2], rk[u][3], sk[u]);
+            *reinterpret_cast<bf16x8*>(d + kto[u][0]) = codes_bf16(rk[u][0], rk[u][1], sk[u]);
+            *reinterpret_cast<bf16x8*>(d + kto[u][1]) = codes_bf16(rk[u][2], rk[u][3], sk[u]);
         }
+        // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
+        if (pos + kTile > len) {
 #pragma unroll
-        for (int u = 0; u < UV; ++u) {
-            const int unit = u * THREADS + threadIdx.x;
-            const int gsel = uniform(unit / DP), x = unit - gsel * DP, hf = x / (DP / 2);
-            // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
-            if (pos + kTile > len) {
+            for (int u = 0; u < UV; ++u)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const int left = len - (pos + gsel * 16 + (hf + 2 * k) * 4);
+                    const int left = len - (pos + group_of(u) * 16 + (hf + 2 * k) * 4);
                     const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
                     rv[u][k][0] &= keep;
                     rv[u][k][1] &= keep;
                 }
-            }
+        }
+#pragma unroll
+        for (int u = 0; u < UV; ++u) {
             const float sc = exp_scale(sv[u] - to < -126 ? -126 : sv[u] - to);
-            f16x8* d = reinterpret_cast<f16x8*>(vd + unit * 32);
-            d[0] = codes_f16(rv[u][0][0], sc, rv[u][1][0], sc);
-            d[1] = codes_f16(rv[u][0][1], sc, rv[u][1][1], sc);
+            *reinterpret_cast<f16x8*>(d + vto[u]) = codes_f16(rv[u][0][0], sc, rv[u][1][0], sc);
+            *reinterpret_cast<f16x8*>(d + vto[u] + 16) = codes_f16(rv[u][0][1], sc, rv[u][1][1], sc);
         }
     };
     f32x16 s[2];
@@ -594,11 +597,11 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         for (int tile = 0; tile < tiles; ++tile) {
             const int pos = lo + tile * kTile;
             if (pos < wave_hi) softmax(pos, refs[0]);
-            if (tile + AHEAD < tiles) keep(tile + AHEAD);
-            if (tile + AHEAD + 1 < tiles) fetch(tile + AHEAD + 1);
-#pragma unroll
-            for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
-            refs[AHEAD - 1] = to;
+            auto next = [&] {
+                if (tile + AHEAD < tiles) keep(tile + AHEAD);
+                if (tile + AHEAD + 1 < tiles) fetch(tile + AHEAD + 1);
+            };
+            if (AHEAD == 1) next();
             lds_barrier();
             if (pos < wave_hi) {
                 // (After the last tile the scores are of a stale one and unused.)
@@ -606,6 +609,10 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
                 scores((tile + 1) % BUFS);
                 operands_ahead<2 * NK + 4 * ND>();
             }
+            if (AHEAD == 2) next();
+#pragma unroll
+            for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
+            refs[AHEAD - 1] = to;
             lds_barrier();
         }
         if (AHEAD == 2 && !behind) lds_barrier();
