@@ -19,6 +19,8 @@
 // Probabilities are rounded to f16 (11 bits, half a step 2^-12: a bf16 probability, 2^-9,
 // would cost as much accuracy as rounding the output) times 2^14, so that they lose nothing
 // before 2^-28.  Maxima, sums and outputs are float32.
+#include <type_traits>
+
 #include "cache_internal.hpp"
 
 namespace occam {
@@ -324,19 +326,9 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Orders a matrix phase of N products: operands are read from LDS kReads products ahead
-// (the compiler by itself reads two and waits for them).
+// A matrix phase reads its operands from LDS this many products ahead (the compiler by
+// itself reads two and waits for them).
 constexpr int kReads = 8;
-template <int N>
-__device__ __forceinline__ void operands_ahead() {
-    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-#pragma unroll
-    for (int i = 0; i < N - kReads; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x8, kReads, 0);
-}
 
 template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
 template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
@@ -346,6 +338,7 @@ template <int DP>
 __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
     constexpr int WAVES = many_waves<DP>(), THREADS = 64 * WAVES, ROWS = 32 * WAVES;
     constexpr int AHEAD = WAVES / 4, BUFS = many_bufs<DP>();
+    constexpr int SETS = WAVES / 4;          // tiles in flight from memory
     constexpr int NK = DP / 16;              // 16-element steps of the score product
     constexpr int ND = DP / 32;              // 32-element tiles of the output
     constexpr int CH = DP / 8;               // 16-byte chunks of a key row in LDS
@@ -432,28 +425,30 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     };
     // A tile on its way from memory to LDS: codes, and what converts them.  Unit x of a
     // group of 16 tokens: 16 codes of a key row; two elements of 8 tokens' values.
-    u32x4 rk[UK];
-    u32x2 rv[UV][2];
-    float sk[UK];
-    int sv[UV], top4 = kMinExp;
+    struct Raw {
+        u32x4 k[UK];
+        u32x2 v[UV][2];
+        float sk[UK];
+        int sv[UV], top;
+    } raw[SETS];
     const int x0 = threadIdx.x % DP, hf = x0 / (DP / 2);
     const unsigned koff = x0 * 16, voff = (hf * DP + (x0 - hf * (DP / 2)) * 2) * 4;
     auto group_of = [&](int u) { return (u * THREADS + wave * 64) / DP; };
-    auto load_tile = [&](int pos, const Win& v) {
+    auto load_tile = [&](int pos, const Win& v, Raw& r) {
         const int g0 = (pos >> 4) & 63;
-        top4 = __builtin_amdgcn_readlane(v.top, g0);
+        r.top = __builtin_amdgcn_readlane(v.top, g0);
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
             const int g = g0 + group_of(u);
-            sk[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v.ks), g));
-            sv[u] = __builtin_amdgcn_readlane(v.ve, g);
+            r.sk[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v.ks), g));
+            r.sv[u] = __builtin_amdgcn_readlane(v.ve, g);
             const size_t off = (unsigned)__builtin_amdgcn_readlane((int)v.lo, g) |
                                (size_t)(unsigned)__builtin_amdgcn_readlane((int)v.hi, g) << 32;
             const unsigned char* kp = a.c.k + off;
             const unsigned char* vp = a.c.v + off;
-            rk[u] = *reinterpret_cast<const u32x4*>(kp + koff);
-            rv[u][0] = *reinterpret_cast<const u32x2*>(vp + voff);
-            rv[u][1] = *reinterpret_cast<const u32x2*>(vp + voff + 2 * DP * 4);
+            r.k[u] = *reinterpret_cast<const u32x4*>(kp + koff);
+            r.v[u][0] = *reinterpret_cast<const u32x2*>(vp + voff);
+            r.v[u][1] = *reinterpret_cast<const u32x2*>(vp + voff + 2 * DP * 4);
         }
     };
     // Where this thread's units go, relative to the buffer.
@@ -467,13 +462,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         kto[u][1] = mrow * DP * 2 + ((c + 1) ^ swz) * 16;
         vto[u] = HALF + unit * 32;
     }
-    auto store_tile = [&](int pos, int buf, int to) {
-        unsigned char* d = lds + buf * 2 * HALF;
-#pragma unroll
-        for (int u = 0; u < UK; ++u) {
-            *reinterpret_cast<bf16x8*>(d + kto[u][0]) = codes_bf16(rk[u][0], rk[u][1], sk[u]);
-            *reinterpret_cast<bf16x8*>(d + kto[u][1]) = codes_bf16(rk[u][2], rk[u][3], sk[u]);
-        }
+    auto mask_tile = [&](int pos, Raw& r) {
         // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
         if (pos + kTile > len) {
 #pragma unroll
@@ -482,43 +471,62 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
                 for (int k = 0; k < 2; ++k) {
                     const int left = len - (pos + group_of(u) * 16 + (hf + 2 * k) * 4);
                     const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-                    rv[u][k][0] &= keep;
-                    rv[u][k][1] &= keep;
+                    r.v[u][k][0] &= keep;
+                    r.v[u][k][1] &= keep;
                 }
         }
-#pragma unroll
-        for (int u = 0; u < UV; ++u) {
-            const float sc = exp_scale(sv[u] - to < -126 ? -126 : sv[u] - to);
-            *reinterpret_cast<f16x8*>(d + vto[u]) = codes_f16(rv[u][0][0], sc, rv[u][1][0], sc);
-            *reinterpret_cast<f16x8*>(d + vto[u] + 16) = codes_f16(rv[u][0][1], sc, rv[u][1][1], sc);
+    };
+    // Part x of four, of unit u.
+    auto store_part = [&](const Raw& r, int buf, int to, int u, int x) {
+        unsigned char* d = lds + buf * 2 * HALF;
+        if (x < 2) {
+            *reinterpret_cast<bf16x8*>(d + kto[u][x]) = codes_bf16(r.k[u][x * 2], r.k[u][x * 2 + 1], r.sk[u]);
+        } else {
+            const float sc = exp_scale(r.sv[u] - to < -126 ? -126 : r.sv[u] - to);
+            *reinterpret_cast<f16x8*>(d + vto[u] + (x - 2) * 16) =
+                codes_f16(r.v[u][0][x - 2], sc, r.v[u][1][x - 2], sc);
         }
+    };
+    auto store_tile = [&](const Raw& r, int buf, int to) {
+#pragma unroll
+        for (int u = 0; u < UK; ++u)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) store_part(r, buf, to, u, x);
     };
     f32x16 s[2];
     f16x8 p[4];
     const int sw = n & (CH < 16 ? CH - 1 : 15);
-    auto scores = [&](int buf) {
-        const unsigned char* kd = lds + buf * 2 * HALF;
+    // The output of the tile in buffer `out` (values times p) and the scores of the one in
+    // `in`, one product after the other; more(i) is other work for after product i.
+    constexpr int OUT = 4 * ND, PRODUCTS = OUT + 2 * NK;
+    auto matrix = [&](auto first, int out, int in, auto&& more) {
+        constexpr int FIRST = decltype(first)::value;
+        const unsigned char* kd = lds + in * 2 * HALF + n * DP * 2;
+        const unsigned char* vd = lds + out * 2 * HALF + HALF + (half * DP + n) * 16;
+        u32x4 f[kReads];
+        auto operand = [&](int i) {
+            if (i < OUT) return *reinterpret_cast<const u32x4*>(vd + (i / ND) * 2 * DP * 16 + (i % ND) * 512);
+            const int c = (i - OUT) / 2, u = (i - OUT) % 2;
+            return *reinterpret_cast<const u32x4*>(kd + u * 32 * DP * 2 + ((c * 2 + half) ^ sw) * 16);
+        };
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int i = FIRST; i < FIRST + kReads; ++i) f[i % kReads] = operand(i);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-#pragma unroll
-        for (int c = 0; c < NK; ++c)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    *reinterpret_cast<const bf16x8*>(kd + (u * 32 + n) * DP * 2 + ((c * 2 + half) ^ sw) * 16),
-                    q[c], s[u], 0, 0, 0);
-    };
-    auto output = [&](int buf) {
-        const unsigned char* vd = lds + buf * 2 * HALF + HALF;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                    *reinterpret_cast<const f16x8*>(vd + ((kk * 2 + half) * DP + d * 32 + n) * 16), p[kk],
-                    acc[d], 0, 0, 0);
+        for (int i = FIRST; i < PRODUCTS; ++i) {
+            if (i < OUT) {
+                acc[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, f[i % kReads]),
+                                                                     p[i / ND], acc[i % ND], 0, 0, 0);
+            } else {
+                const int c = (i - OUT) / 2, u = (i - OUT) % 2;
+                f32x16 z = {};
+                if (c) z = s[u];
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[i % kReads]), q[c], z,
+                                                               0, 0, 0);
+            }
+            if (i + kReads < PRODUCTS) f[i % kReads] = operand(i + kReads);
+            more(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     auto softmax = [&](int pos, int refs) {
         // The first of the wave's rows sees up to 31 keys fewer than the last.
@@ -571,49 +579,76 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         win.page = win_page(base);
         win_scales(base, win);
         nxt = win;
-        auto fetch = [&](int tile) {
-            const int pos = lo + tile * kTile, in = (pos >> 4) & 63;
-            if (((pos >> 4) & ~63) != base) { win = nxt; base += 64; }
-            load_tile(pos, win);
+        // Tiles past the last one are fetched (page 0's codes) and stored like the others, so
+        // that a matrix phase has no branches; nothing reads them.
+        auto window = [&](int tile) {
+            const int in = ((lo + tile * kTile) >> 4) & 63;
+            if (((lo + tile * kTile) >> 4 & ~63) != base) { win = nxt; base += 64; }
             if (in == 0 || tile == 0) nxt.page = win_page(base + 64);
             if (in == 32 || (tile == 0 && in > 32)) win_scales(base + 64, nxt);
         };
+        auto fetch = [&](int tile, Raw& r) { load_tile(lo + tile * kTile, win, r); };
         int refs[AHEAD + 1];                     // of tiles t .. t + AHEAD
         int to = kMinExp;
-        auto keep = [&](int tile) {
-            to = top4 > to ? top4 : to;
-            store_tile(lo + tile * kTile, tile % BUFS, to);
-        };
         for (int x = 0; x < AHEAD; ++x) {
-            if (x < tiles) { fetch(x); keep(x); }
+            window(x);
+            fetch(x, raw[0]);
+            mask_tile(lo + x * kTile, raw[0]);
+            to = raw[0].top > to ? raw[0].top : to;
+            store_tile(raw[0], x % BUFS, to);
             refs[x] = to;
         }
-        if (AHEAD < tiles) fetch(AHEAD);         // in flight until the next vector phase
+#pragma unroll
+        for (int x = 0; x < SETS; ++x) {
+            window(AHEAD + x);
+            fetch(AHEAD + x, raw[x]);
+        }
         lds_barrier();
         const bool behind = AHEAD == 2 && wave >= 4;
         if (behind) lds_barrier();
-        scores(0);
+        const auto nothing = [](int) {};
+        const std::integral_constant<int, 0> all;
+        matrix(std::integral_constant<int, OUT>{}, 0, 0, nothing);
         lds_barrier();
-        for (int tile = 0; tile < tiles; ++tile) {
-            const int pos = lo + tile * kTile;
+        // One tile: `r` holds tile + AHEAD, and tile + AHEAD + SETS afterwards.
+        auto step = [&](int tile, Raw& r) {
+            const int pos = lo + tile * kTile, to_store = (tile + AHEAD) % BUFS;
             if (pos < wave_hi) softmax(pos, refs[0]);
-            auto next = [&] {
-                if (tile + AHEAD < tiles) keep(tile + AHEAD);
-                if (tile + AHEAD + 1 < tiles) fetch(tile + AHEAD + 1);
-            };
-            if (AHEAD == 1) next();
-            lds_barrier();
-            if (pos < wave_hi) {
-                // (After the last tile the scores are of a stale one and unused.)
-                output(tile % BUFS);
-                scores((tile + 1) % BUFS);
-                operands_ahead<2 * NK + 4 * ND>();
+            if (AHEAD == 1) {
+                mask_tile(pos + kTile, r);
+                to = r.top > to ? r.top : to;
+                store_tile(r, to_store, to);
+                window(tile + 1 + SETS);
+                fetch(tile + 1 + SETS, r);
             }
-            if (AHEAD == 2) next();
+            lds_barrier();
+            // (After the last tile the scores are of a stale one and unused.)
+            if (AHEAD == 1) {
+                if (pos < wave_hi) matrix(all, tile % BUFS, (tile + 1) % BUFS, nothing);
+            } else {
+                __builtin_amdgcn_s_setprio(1);
+                mask_tile(pos + 2 * kTile, r);
+                window(tile + 2 + SETS);
+                to = r.top > to ? r.top : to;
+                if (pos < wave_hi) {
+                    matrix(all, tile % BUFS, (tile + 1) % BUFS, [&](int i) {
+                        if (i % 2 == 0 && i < 8) store_part(r, to_store, to, 0, i / 2);
+                        if (i == 9) fetch(tile + 2 + SETS, r);
+                    });
+                } else {
+                    store_tile(r, to_store, to);
+                    fetch(tile + 2 + SETS, r);
+                }
+                __builtin_amdgcn_s_setprio(0);
+            }
 #pragma unroll
             for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
             refs[AHEAD - 1] = to;
             lds_barrier();
+        };
+        for (int tile = 0; tile < tiles; tile += SETS) {
+            step(tile, raw[0]);
+            if (SETS == 2 && tile + 1 < tiles) step(tile + 1, raw[SETS - 1]);
         }
         if (AHEAD == 2 && !behind) lds_barrier();
     }
