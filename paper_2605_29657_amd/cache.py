@@ -108,19 +108,22 @@ def lib():
     return _lib
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _enqueue(fn, device, stream, *args):
     """Call ``fn(*args, stream)`` with ``device`` current and raise on an error status."""
     index = device.index
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
+        stream = _raw_stream(index)
     elif isinstance(stream, torch.cuda.Stream):
         stream = stream.cuda_stream
-    if index is None or index == torch.cuda.current_device():
+    if index == torch.cuda.current_device():
         st = fn(*args, stream)
     else:
         with torch.cuda.device(device):
             st = fn(*args, stream)
-    if st != occam.OK:
+    if st:
         raise occam.OccamError(st, occam.status_string(st))
 
 
@@ -128,22 +131,25 @@ def _bad(msg):
     raise occam.OccamError(occam.ERR_INVALID_ARG, msg)
 
 
+_I32, _F32 = torch.int32, torch.float32
+
+
 def _ints(t, device, name, at_least=0):
     """Pointer of an int32 device vector (None stays None)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous() or t.numel() < at_least:
+    if t.dtype is not _I32 or t.device != device or not t.is_contiguous() or t.numel() < at_least:
         _bad("%s must be a contiguous int32 tensor on %s with at least %d elements" % (name, device, at_least))
     return t.data_ptr()
 
 
-def _rows(t, device, name, heads, dim, dtypes):
+def _rows(t, device, name, heads, dim, dtype):
     """(pointer, row stride) of a tensor [rows, heads, dim] whose heads are packed."""
-    if (t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.device != device or
-            t.dtype not in dtypes or (t.shape[0] and (t.stride(2) != 1 and dim > 1 or t.stride(1) != dim and heads > 1))):
-        _bad("%s must be a [rows, %d, %d] tensor on %s with packed heads, of %s" % (
-            name, heads, dim, device, " or ".join(str(d) for d in dtypes)))
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * dim)
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3 and shape[1] == heads and shape[2] == dim and t.dtype is dtype and t.device == device:
+        if not shape[0] or ((stride[2] == 1 or dim == 1) and (stride[1] == dim or heads == 1)):
+            return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * dim)
+    _bad("%s must be a [rows, %d, %d] tensor of %s on %s with packed heads" % (name, heads, dim, dtype, device))
 
 
 _DTYPES = {torch.float32: occam.F32, torch.bfloat16: occam.BF16}
@@ -188,19 +194,19 @@ def rotate(rotary, positions, src, dst=None, inverse=False, stream=None):
         _bad("src and dst must be lists of 1 to %d tensors" % occam.MAX_ROW_TENSORS)
     x = src[0]
     dev, dt, rows, d = x.device, x.dtype, x.shape[0], rotary.head_dim
-    if dt not in _DTYPES or positions.numel() != rows * rotary.axes:
-        _bad("positions must have %d axes for every row, tensors float32 or bfloat16" % rotary.axes)
-    arr = (_Heads * len(src))()
-    for i, (s, o) in enumerate(zip(src, dst)):
-        if s.shape[0] != rows or o.shape != s.shape:
+    if dt not in _DTYPES or dev.type != "cuda" or positions.numel() != rows * rotary.axes:
+        _bad("positions must have %d axes for every row, tensors float32 or bfloat16 on a GPU" % rotary.axes)
+    heads = []
+    for t, o in zip(src, dst):
+        if t.dim() != 3 or t.shape[0] != rows or o.shape != t.shape:
             _bad("every tensor must have the same rows")
-        arr[i].src, arr[i].src_row_stride = _rows(s, dev, "src", s.shape[1], d, (dt,))
-        arr[i].dst, arr[i].dst_row_stride = _rows(o, dev, "dst", s.shape[1], d, (dt,))
-        arr[i].heads = s.shape[1]
+        n = t.shape[1]
+        (ps, ss), (pd, sd) = _rows(t, dev, "src", n, d, dt), _rows(o, dev, "dst", n, d, dt)
+        heads.append((ps, pd, n, ss, sd))
     if rows == 0:
         return
     _enqueue(lib().occam_rotate, dev, stream, rotary.ref, rows, _ints(positions, dev, "positions"),
-             1 if inverse else 0, _DTYPES[dt], len(src), arr)
+             1 if inverse else 0, _DTYPES[dt], len(heads), (_Heads * len(heads))(*heads))
 
 
 # ------------------------------------------------------------------------------- pages
@@ -258,21 +264,23 @@ class Batch:
     def __init__(self, n, rows=1, seq=None, row_offsets=None, max_rows=0):
         self.n, self.seq, self.row_offsets = int(n), seq, row_offsets     # kept alive
         self.rows = int(rows)
+        self.device = None
         for t, least, name in ((seq, self.n, "seq"), (row_offsets, self.n + 1, "row_offsets")):
             if t is not None:
-                _ints(t, t.device, name, least)
+                self.device = t.device if self.device is None else self.device
+                _ints(t, self.device, name, least)
         self.c = _Batch(self.n, None if seq is None else seq.data_ptr(), self.rows,
                         None if row_offsets is None else row_offsets.data_ptr(), int(max_rows))
         self.ref = ctypes.byref(self.c)
 
-    def check(self, device, tensors=()):
-        for t in (self.seq, self.row_offsets):
-            if t is not None and t.device != device:
-                _bad("the batch's tensors must be on %s" % device)
+    def check(self, device, *tensors):
+        if self.device is not None and self.device != device:
+            _bad("the batch's tensors must be on %s" % device)
         if self.row_offsets is None:
+            least = self.n * self.rows
             for t in tensors:
-                if t is not None and t.shape[0] < self.n * self.rows:
-                    _bad("the batch has %d rows, a tensor %d" % (self.n * self.rows, t.shape[0]))
+                if t is not None and t.shape[0] < least:
+                    _bad("the batch has %d rows, a tensor %d" % (least, t.shape[0]))
 
 
 def plan(pages, n):
@@ -320,11 +328,11 @@ def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=
 def append(pages, layer, batch, plan, k, v, stream=None):
     """occam_cache_append: ``k`` and ``v`` [rows, num_kv_heads, head_dim], float32 or bfloat16."""
     dev = pages.device
-    batch.check(dev, (k, v))
+    batch.check(dev, k, v)
     if k.dtype != v.dtype or k.dtype not in _DTYPES or k.shape[0] != v.shape[0]:
         _bad("k and v must have the same rows and be both float32 or both bfloat16")
-    kp = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, (k.dtype,))
-    vp = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, (k.dtype,))
+    kp = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, k.dtype)
+    vp = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, k.dtype)
     if k.shape[0] == 0:
         return
     _enqueue(lib().occam_cache_append, dev, stream, pages.ref, layer.ref, batch.ref, *_plan(pages, plan),
@@ -334,13 +342,13 @@ def append(pages, layer, batch, plan, k, v, stream=None):
 def read(pages, layer, batch, k, v=None, start=None, stream=None):
     """occam_cache_read into ``k`` and ``v`` (either may be None), float32 or bfloat16."""
     dev = pages.device
-    batch.check(dev, (k, v))
+    batch.check(dev, k, v)
     x = k if k is not None else v
     if x is None or x.dtype not in _DTYPES:
         _bad("k or v must be a float32 or bfloat16 tensor")
     ptrs = []
     for t, name in ((k, "k"), (v, "v")):
-        ptrs += (None, 0) if t is None else _rows(t, dev, name, layer.num_kv_heads, layer.head_dim, (x.dtype,))
+        ptrs += (None, 0) if t is None else _rows(t, dev, name, layer.num_kv_heads, layer.head_dim, x.dtype)
     if x.shape[0] == 0:
         return
     _enqueue(lib().occam_cache_read, dev, stream, pages.ref, layer.ref, batch.ref,
@@ -373,12 +381,12 @@ def attend(pages, layer, batch, q, out, ws, lse=None, causal=True, softmax_scale
     """occam_cache_attend: ``q`` and ``out`` bfloat16 [rows, num_heads, head_dim], ``lse``
     float32 [rows, num_heads] or None."""
     dev, H = pages.device, q.shape[1]
-    batch.check(dev, (q, out, lse))
-    qp = _rows(q, dev, "q", H, layer.head_dim, (torch.bfloat16,))
-    op = _rows(out, dev, "out", H, layer.head_dim, (torch.bfloat16,))
+    batch.check(dev, q, out, lse)
+    qp = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)
+    op = _rows(out, dev, "out", H, layer.head_dim, torch.bfloat16)
     if q.shape[0] != out.shape[0] or ws.device != dev:
         _bad("q and out must have the same rows, and the workspace the pages' device")
-    if lse is not None and (lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous() or
+    if lse is not None and (lse.dtype is not _F32 or lse.device != dev or not lse.is_contiguous() or
                             lse.numel() < q.shape[0] * H):
         _bad("lse must be a contiguous float32 tensor [rows, %d] on %s" % (H, dev))
     if q.shape[0] == 0:
