@@ -699,28 +699,49 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows)
     const int T = row_count(a.b, i), slot = slot_of(a.b, i);
     if (t >= T) return;
     const int len = slot >= 0 && slot < a.pg.num_seqs ? a.pg.length[slot] : 0;
+    const long long orow = (long long)row_begin(a.b, i) + t;
+    const size_t at = ((size_t)orow * a.H + hh) * a.splits;
+    const int te = threadIdx.x % TE, grp = threadIdx.x / TE;
+    const bool in = te * 4 < a.c.d;
+    // The first splits of every group are read before anything is known of the
+    // sequence (what a split that does not exist left there is not used).
+    constexpr int AHEAD = 4;
+    float pl[AHEAD], l0 = -INFINITY;
+    f32x4 po[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+        const int p = grp + k * NG;
+        pl[k] = p < a.splits ? a.part_l[at + p] : -INFINITY;
+        po[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (in && p < a.splits) po[k] = *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
+    }
+    if (lane < a.splits) l0 = a.part_l[at + lane];
     // The keys of the row block that the row was computed in decide which splits exist.
     const int r = t * a.g + hh % a.g, r1 = (r / block_rows + 1) * block_rows - 1;
     const int tm = r1 / a.g < T - 1 ? r1 / a.g : T - 1;
     const int end = a.causal ? len - T + tm + 1 : len;
     int parts = end > 0 ? (end + a.chunk - 1) / a.chunk : 1;
     parts = parts < a.splits ? parts : a.splits;
-    const long long orow = (long long)row_begin(a.b, i) + t;
-    const size_t at = ((size_t)orow * a.H + hh) * a.splits;
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_l[at + p]);
+    float top = lane < parts ? l0 : -INFINITY;
+    for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, a.part_l[at + p]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float base = top == -INFINITY ? 0.f : top;
-    const int te = threadIdx.x % TE, grp = threadIdx.x / TE;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f;
-    const bool in = te * 4 < a.c.d;
-#pragma unroll 4
-    for (int p = grp; p < parts; p += NG) {
-        const float wgt = __builtin_amdgcn_exp2f(a.part_l[at + p] - base);
+    auto add = [&](int p, float pl, f32x4 po) {
+        if (p >= parts) return;
+        const float wgt = __builtin_amdgcn_exp2f(pl - base);
         sum += wgt;
-        if (in) y += wgt * *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
+        y += wgt * po;
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) add(grp + k * NG, pl[k], po[k]);
+#pragma unroll 4
+    for (int p = grp + AHEAD * NG; p < parts; p += NG) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (in) x = *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
+        add(p, a.part_l[at + p], x);
     }
     jo[grp][te] = y;
     if (te == 0) js[grp] = sum;

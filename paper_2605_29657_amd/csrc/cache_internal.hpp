@@ -41,10 +41,10 @@ __device__ __forceinline__ int row_count(const BatchView& b, int i) {
     return r < 0 ? 0 : r < b.max_rows ? r : b.max_rows;
 }
 
-// The plan: a header of four ints (kind, n, page items, 0), arrays of n + 1 ints, and for
-// keep a page list of max_pages ints per sequence.
+// The plan: a header of four ints (kind, n, page items, 0), arrays of n + 1 ints, for keep
+// a page list of max_pages ints per sequence, and the sequence of every page item.
 //   reserve: ITEMS prefix of the pages that receive rows, FIRST tokens held before,
-//            TAIL page that holds the partly filled last page's tokens (or -1), ROWS
+//            TAIL page that holds the partly filled last page's tokens (or -1), ROWS, SLOT
 //   keep:    ITEMS prefix of the pages rewritten, FIRST page rewritten, OLD tokens before,
 //            NEW tokens after, START and SPAN of the span, SLOT
 //   fork:    ITEMS tokens of the source, or -1 where the call failed
@@ -54,7 +54,7 @@ enum { PL_ITEMS = 0, PL_FIRST = 1, PL_TAIL = 2, PL_ROWS = 3, PL_OLD = 2, PL_NEW 
        PL_SPAN = 5, PL_SLOT = 6 };
 
 __host__ __device__ inline size_t plan_ints(int n, int max_pages) {
-    return kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages;
+    return kPlanHeader + (size_t)kPlanArrays * (n + 1) + 2 * (size_t)n * max_pages;
 }
 __device__ __forceinline__ int* plan_array(int* plan, int n, int a) {
     return plan + kPlanHeader + (size_t)a * (n + 1);
@@ -67,6 +67,13 @@ __device__ __forceinline__ int* plan_pages(int* plan, int n, int max_pages, int 
 }
 __device__ __forceinline__ const int* plan_pages(const int* plan, int n, int max_pages, int i) {
     return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)i * max_pages;
+}
+// The sequence of every page item (at most n * max_pages of them).
+__device__ __forceinline__ int* plan_owner(int* plan, int n, int max_pages) {
+    return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages;
+}
+__device__ __forceinline__ const int* plan_owner(const int* plan, int n, int max_pages) {
+    return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages;
 }
 // The last i in [0, n) with prefix[i] <= x: the sequence that item x belongs to.
 __device__ __forceinline__ int owner_of(const int* prefix, int n, int x) {

@@ -7,6 +7,8 @@
 // (page, key head) block of keys or of values has U = page_tokens * dp / 32 units (32 to
 // 2048) and one scale; a workgroup of 256 threads takes 256 / U blocks at a time, or one
 // block with U / 256 units per thread.
+#include <type_traits>
+
 #include "cache_internal.hpp"
 
 namespace occam {
@@ -73,21 +75,23 @@ __device__ __forceinline__ void store_codes(unsigned char* blk, bool val, int dp
     }
 }
 
+// Eight elements of a row as they lie in memory, and as float32.
 template <bool F32>
-__device__ __forceinline__ void load_row8(const char* p, float* x) {
-    if constexpr (F32) {
-        const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-    } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-        }
+struct Row8 {
+    u32x4 w[F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const char* p) {
+        w[0] = reinterpret_cast<const u32x4*>(p)[0];
+        if constexpr (F32) w[1] = reinterpret_cast<const u32x4*>(p)[1];
     }
-}
+    __device__ __forceinline__ void zero() {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (F32) w[1] = u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (F32) return __uint_as_float(w[e >> 2][e & 3]);
+        return __uint_as_float(e & 1 ? w[0][e >> 1] & 0xffff0000u : w[0][e >> 1] << 16);
+    }
+};
 
 // One (page, head) block of keys (kv = 0) or values (kv = 1) of an item.
 struct Block {
@@ -105,24 +109,31 @@ __device__ __forceinline__ Block block_at(int w, int items, int Hkv) {
     return b;
 }
 
-template <bool F32>
+// UPT units per thread.  Up to two are held in registers between the search for the
+// largest magnitude and the conversion; larger blocks are read a second time (from L2).
+template <bool F32, int UPT>
 __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheView c, BatchView b,
                                                             const int* plan, const char* k,
                                                             long long kst, const char* v,
                                                             long long vst) {
+    constexpr bool KEEP = UPT <= 2;
     __shared__ float red[kRowThreads / 64];
-    if (plan[0] != kPlanReserve || plan[1] != b.n) return;
-    const int n = b.n, items = plan[2], G = 1 << p.shift;
+    const int n = b.n, G = 1 << p.shift;
+    if (plan[0] != kPlanReserve || plan[1] != n) return;
+    const int items = plan[2];
     const int* pre = plan_array(plan, n, PL_ITEMS);
+    const int* owner = plan_owner(plan, n, p.max_pages);
     const int units = (G >> 2) * (c.dp >> 3), span = units < kRowThreads ? units : kRowThreads;
     const int side = kRowThreads / span;                 // blocks of this workgroup at a time
-    const int chunks = c.dp >> 3, total = items * c.Hkv * 2;
+    const int shift = c.dp == 64 ? 3 : c.dp == 128 ? 4 : 5;            // units per group of tokens
+    const int total = items * c.Hkv * 2;
+    constexpr int ESZ = F32 ? 4 : 2;
     for (int w0 = blockIdx.x * side; w0 < total; w0 += gridDim.x * side) {
         const Block bl = block_at(w0 + threadIdx.x / span, items, c.Hkv);
-        const int i = owner_of(pre, n, bl.item);
+        const int i = owner[bl.item];
         const int len = plan_array(plan, n, PL_FIRST)[i], rows = plan_array(plan, n, PL_ROWS)[i];
         const int j = (len >> p.shift) + bl.item - pre[i];
-        const int page = p.table[(size_t)slot_of(b, i) * p.max_pages + j];
+        const int page = p.table[(size_t)plan_array(plan, n, PL_SLOT)[i] * p.max_pages + j];
         const int pos0 = j << p.shift;
         const int had = len > pos0 ? len - pos0 : 0;     // tokens the page held
         const int tail = had ? plan_array(plan, n, PL_TAIL)[i] : page;
@@ -130,26 +141,31 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
         unsigned char* blk = (bl.kv ? c.v : c.k) + at * c.block;
         const unsigned char* src = (bl.kv ? c.v : c.k) + from * c.block;
         float* scale = bl.kv ? c.vs : c.ks;
-        const int e_sz = F32 ? 4 : 2;
-        const char* x = (bl.kv ? v : k);
         const long long st = bl.kv ? vst : kst;
-        const long long row0 = (long long)row_begin(b, i) - len + pos0;    // of the page's token 0
+        // Row of the page's token 0 in the packed rows, at this head.
+        const char* x = (bl.kv ? v : k) +
+                        (((long long)row_begin(b, i) - len + pos0) * st + (long long)bl.head * c.d) * ESZ;
         const int end = len + rows - pos0 < G ? len + rows - pos0 : G;     // tokens it holds now
-        float top = 0.f;
-        if (bl.live)
-            for (int u = threadIdx.x % span; u < units; u += span) {
-                const int quad = u / chunks, e0 = (u - quad * chunks) * 8;
-                if (e0 >= c.d || quad * 4 + 3 < had || quad * 4 >= end) continue;
+        Row8<F32> raw[KEEP ? UPT : 1][4];
+        auto load = [&](int u, Row8<F32>* r) {
+            const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int tok = quad * 4 + t;
-                    if (tok < had || tok >= end) continue;
-                    float y[8];
-                    load_row8<F32>(x + ((row0 + tok) * st + (long long)bl.head * c.d + e0) * e_sz, y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(y[e]));
-                }
+            for (int t = 0; t < 4; ++t) {
+                const int tok = quad * 4 + t;
+                if (bl.live && e0 < c.d && tok >= had && tok < end) r[t].load(x + (tok * st + e0) * ESZ);
+                else r[t].zero();
             }
+        };
+        float top = 0.f;
+#pragma unroll
+        for (int y = 0; y < UPT; ++y) {
+            Row8<F32>* r = raw[KEEP ? y : 0];
+            load(y * span + threadIdx.x % span, r);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(r[t].at(e)));
+        }
         top = group_max(top, span, red);
         const int oldexp = had ? exp_of(scale[from]) : kMinExp;
         const int newexp = scale_exp(top) > oldexp ? scale_exp(top) : oldexp;
@@ -158,31 +174,23 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
         const float again = exp_scale(oldexp - newexp < -126 ? -126 : oldexp - newexp);
         const bool rewrite = had && (tail != page || newexp != oldexp);
         if (bl.live)
-            for (int u = threadIdx.x % span; u < units; u += span) {
-                const int quad = u / chunks, e0 = (u - quad * chunks) * 8;
+#pragma unroll
+            for (int y = 0; y < UPT; ++y) {
+                const int u = y * span + threadIdx.x % span;
+                const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
                 if (quad * 4 >= end || (quad * 4 + 3 < had && !rewrite)) continue;
-                float y[32] = {};
-                if (quad * 4 < had) {
-                    load_codes(src, bl.kv, c.dp, quad, e0, y);
+                Row8<F32>* r = raw[KEEP ? y : 0];
+                if (!KEEP) load(u, r);
+                float z[32] = {};
+                if (quad * 4 < had) load_codes(src, bl.kv, c.dp, quad, e0, z);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[t * 8 + e] = quad * 4 + t < had ? y[t * 8 + e] * again : 0.f;
-                }
-                if (e0 < c.d) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int tok = quad * 4 + t;
-                        if (tok < had || tok >= end) continue;
-                        load_row8<F32>(x + ((row0 + tok) * st + (long long)bl.head * c.d + e0) * e_sz,
-                                       y + t * 8);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[t * 8 + e] = __builtin_amdgcn_fmed3f(y[t * 8 + e] * inv, -most, most);
-                    }
-                }
-                store_codes(blk, bl.kv, c.dp, quad, e0, y);
+                    for (int e = 0; e < 8; ++e)
+                        z[t * 8 + e] = quad * 4 + t < had
+                                           ? z[t * 8 + e] * again
+                                           : __builtin_amdgcn_fmed3f(r[t].at(e) * inv, -most, most);
+                store_codes(blk, bl.kv, c.dp, quad, e0, z);
             }
         // Every thread of the block has read scale[from], which is scale[at] where the page
         // stays the sequence's own.
@@ -253,6 +261,9 @@ __device__ __forceinline__ int source_of(const Kept& s, int x) {
     return s.start + v;
 }
 
+// Codes and their scales stay in registers between the search and the conversion (12 per
+// unit).
+template <int UPT>
 __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView c, int n,
                                                           const int* plan, const int* idx,
                                                           const int* off) {
@@ -260,11 +271,13 @@ __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView 
     if (plan[0] != kPlanKeep || plan[1] != n) return;
     const int items = plan[2], G = 1 << p.shift;
     const int* pre = plan_array(plan, n, PL_ITEMS);
+    const int* owner = plan_owner(plan, n, p.max_pages);
     const int units = (G >> 2) * (c.dp >> 3), span = units < kRowThreads ? units : kRowThreads;
-    const int side = kRowThreads / span, chunks = c.dp >> 3, total = items * c.Hkv * 2;
+    const int shift = c.dp == 64 ? 3 : c.dp == 128 ? 4 : 5;
+    const int side = kRowThreads / span, total = items * c.Hkv * 2;
     for (int w0 = blockIdx.x * side; w0 < total; w0 += gridDim.x * side) {
         const Block bl = block_at(w0 + threadIdx.x / span, items, c.Hkv);
-        const int i = owner_of(pre, n, bl.item);
+        const int i = owner[bl.item];
         const int first = plan_array(plan, n, PL_FIRST)[i], now = plan_array(plan, n, PL_NEW)[i];
         const int* olds = plan_pages(plan, n, p.max_pages, i);
         const int j = first + bl.item - pre[i];
@@ -274,64 +287,75 @@ __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView 
         const int page = p.table[(size_t)plan_array(plan, n, PL_SLOT)[i] * p.max_pages + j];
         unsigned char* store = bl.kv ? c.v : c.k;
         float* scale = bl.kv ? c.vs : c.ks;
-        // Eight codes of the token that becomes token tok of this page, and their scale.
-        auto fetch = [&](int tok, int e0, float* y) -> float {
-            const int from = source_of(kept, pos0 + tok), in = from & (G - 1);
-            const size_t at = (size_t)olds[from >> p.shift] * c.Hkv + bl.head;
-            const unsigned char* blk = store + at * c.block;
-            if (bl.kv) {
-                const unsigned char* w = blk + ((size_t)(in >> 2) * c.dp + e0) * 4;
-                const u32x4 a = reinterpret_cast<const u32x4*>(w)[0];
-                const u32x4 b = reinterpret_cast<const u32x4*>(w)[1];
-                const int sh = (in & 3) * 8;
-                unsigned lo = 0, hi = 0;
+        u32x2 code[UPT][4];                     // eight codes of a token
+        float sc[UPT][4], top = 0.f;
+        // Where the tokens come from, then their codes and scales, all at once.
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    lo |= (a[e] >> sh & 255u) << (8 * e);
-                    hi |= (b[e] >> sh & 255u) << (8 * e);
-                }
-                const f32x4 q = dec4(lo), r = dec4(hi);
+        for (int y = 0; y < UPT; ++y) {
+            const int u = y * span + threadIdx.x % span;
+            const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
+            int from[4];
+            size_t at[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { y[e] = q[e]; y[4 + e] = r[e]; }
-            } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(blk + (size_t)in * c.dp + e0);
-                const f32x4 q = dec4(w[0]), r = dec4(w[1]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { y[e] = q[e]; y[4 + e] = r[e]; }
+            for (int t = 0; t < 4; ++t) {
+                const int tok = quad * 4 + t;
+                from[t] = bl.live && tok < end ? source_of(kept, pos0 + tok) : -1;
             }
-            return scale[at];
-        };
-        float top = 0.f;
-        if (bl.live)
-            for (int u = threadIdx.x % span; u < units; u += span) {
-                const int quad = u / chunks, e0 = (u - quad * chunks) * 8;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (quad * 4 + t >= end) continue;
-                    float y[8], m = 0.f;
-                    const float sc = fetch(quad * 4 + t, e0, y);
+            for (int t = 0; t < 4; ++t)
+                at[t] = from[t] < 0 ? 0 : (size_t)olds[from[t] >> p.shift] * c.Hkv + bl.head;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
-                    top = fmaxf(top, m * sc);
+            for (int t = 0; t < 4; ++t) {
+                code[y][t] = u32x2{0, 0};
+                sc[y][t] = 1.f;
+                if (from[t] < 0) continue;
+                sc[y][t] = scale[at[t]];
+                const int in = from[t] & (G - 1);
+                const unsigned char* blk = store + at[t] * c.block;
+                if (bl.kv) {
+                    const unsigned char* w = blk + ((size_t)(in >> 2) * c.dp + e0) * 4;
+                    const u32x4 a = reinterpret_cast<const u32x4*>(w)[0];
+                    const u32x4 b = reinterpret_cast<const u32x4*>(w)[1];
+                    const int sh = (in & 3) * 8;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        code[y][t][0] |= (a[e] >> sh & 255u) << (8 * e);
+                        code[y][t][1] |= (b[e] >> sh & 255u) << (8 * e);
+                    }
+                } else {
+                    code[y][t] = *reinterpret_cast<const u32x2*>(blk + (size_t)in * c.dp + e0);
                 }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < UPT; ++y)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const f32x4 q = dec4(code[y][t][0]), r = dec4(code[y][t][1]);
+                float m = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(q[e]), fabsf(r[e])));
+                top = fmaxf(top, m * sc[y][t]);
             }
         top = group_max(top, span, red);
         const int newexp = scale_exp(top);
         if (!bl.live) continue;
-        for (int u = threadIdx.x % span; u < units; u += span) {
-            const int quad = u / chunks, e0 = (u - quad * chunks) * 8;
+#pragma unroll
+        for (int y = 0; y < UPT; ++y) {
+            const int u = y * span + threadIdx.x % span;
+            const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
             if (quad * 4 >= end) continue;
-            float y[32] = {};
+            float z[32];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                if (quad * 4 + t >= end) continue;
-                int d = exp_of(fetch(quad * 4 + t, e0, y + t * 8)) - newexp;
+                int d = exp_of(sc[y][t]) - newexp;
                 d = d < -126 ? -126 : d > 127 ? 127 : d;       // 127: a block of zeros
                 const float f = exp_scale(d);
+                const f32x4 q = dec4(code[y][t][0]), r = dec4(code[y][t][1]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[t * 8 + e] *= f;
+                for (int e = 0; e < 4; ++e) { z[t * 8 + e] = q[e] * f; z[t * 8 + 4 + e] = r[e] * f; }
             }
-            store_codes(store + ((size_t)page * c.Hkv + bl.head) * c.block, bl.kv, c.dp, quad, e0, y);
+            store_codes(store + ((size_t)page * c.Hkv + bl.head) * c.block, bl.kv, c.dp, quad, e0, z);
         }
         if (threadIdx.x % span == 0) scale[(size_t)page * c.Hkv + bl.head] = exp_scale(newexp);
     }
@@ -346,6 +370,17 @@ int row_grid(const PageView& p, const CacheView& c, long long blocks) {
     return (int)(wgs < 4096 ? wgs : 4096);
 }
 
+// Calls f(UPT) with the units per thread of a block as a compile-time number.
+template <typename F>
+hipError_t with_units(const PageView& p, const CacheView& c, F f) {
+    switch ((1 << p.shift) / 4 * (c.dp / 8) / kRowThreads) {
+        case 8: return f(std::integral_constant<int, 8>{});
+        case 4: return f(std::integral_constant<int, 4>{});
+        case 2: return f(std::integral_constant<int, 2>{});
+        default: return f(std::integral_constant<int, 1>{});
+    }
+}
+
 }  // namespace
 
 hipError_t launch_cache_append(const PageView& p, const CacheView& c, const BatchView& b,
@@ -355,8 +390,11 @@ hipError_t launch_cache_append(const PageView& p, const CacheView& c, const Batc
     const long long pages = (long long)b.n * (((most - 1) >> p.shift) + 2);
     const dim3 grid(row_grid(p, c, pages * c.Hkv * 2));
     auto kk = static_cast<const char*>(k), vv = static_cast<const char*>(v);
-    return f32 ? launch(cache_append<true>, grid, dim3(kRowThreads), 0, s, p, c, b, plan, kk, ks, vv, vs)
-               : launch(cache_append<false>, grid, dim3(kRowThreads), 0, s, p, c, b, plan, kk, ks, vv, vs);
+    return with_units(p, c, [&](auto upt) {
+        constexpr int U = decltype(upt)::value;
+        return f32 ? launch(cache_append<true, U>, grid, dim3(kRowThreads), 0, s, p, c, b, plan, kk, ks, vv, vs)
+                   : launch(cache_append<false, U>, grid, dim3(kRowThreads), 0, s, p, c, b, plan, kk, ks, vv, vs);
+    });
 }
 
 hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchView& b,
@@ -374,8 +412,10 @@ hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const
                              const int* idx, const int* off, hipStream_t s) {
     long long pages = (long long)n * p.max_pages;
     if (pages > p.num_pages) pages = p.num_pages;
-    return launch(cache_move, dim3(row_grid(p, c, pages * c.Hkv * 2)), dim3(kRowThreads), 0, s, p, c,
-                  n, plan, idx, off);
+    const dim3 grid(row_grid(p, c, pages * c.Hkv * 2));
+    return with_units(p, c, [&](auto upt) {
+        return launch(cache_move<decltype(upt)::value>, grid, dim3(kRowThreads), 0, s, p, c, n, plan, idx, off);
+    });
 }
 
 }  // namespace occam

@@ -14,7 +14,10 @@
 namespace occam {
 namespace {
 
-constexpr int kPlanThreads = 1024;
+// Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences (fewer
+// waves at every barrier), 1024 beyond.  What a call reads again of its sequences is kept in
+// LDS for up to kNear of them, in the plan beyond.
+constexpr int kNear = 1024;
 
 // Exclusive prefix of x over the workgroup (NT threads), and the total.
 template <int NT>
@@ -41,21 +44,23 @@ __device__ __forceinline__ int block_scan(int x, int* total, int* red) {
 }
 
 struct PlanShared {
-    int need[OCCAM_MAX_BATCH + 1];         // prefix of the pages wanted
+    int need[OCCAM_MAX_BATCH + 1];         // a prefix over the call's sequences
     unsigned seen[OCCAM_MAX_SLOTS / 32];   // slots of the call
-    int red[kPlanThreads / 64];
+    int near[4][kNear];
+    int list[kNear];                       // pages taken, by rank
+    int red[16];
     int bad;
 };
 static_assert(sizeof(PlanShared) <= 65536, "plan state exceeds the default LDS limit");
 
-// Prefix of the values that get(i) gives for i in [0, n) into out[0 .. n] (LDS or global).
-template <typename F>
+// Prefix of the values that get(i) gives for i in [0, n) into out[0 .. n].
+template <int NT, typename F>
 __device__ __forceinline__ int prefix_of(int n, int* out, int* red, F get) {
     int base = 0;
-    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    for (int i0 = 0; i0 < n; i0 += NT) {
         const int i = i0 + threadIdx.x;
         int total;
-        const int at = block_scan<kPlanThreads>(i < n ? get(i) : 0, &total, red);
+        const int at = block_scan<NT>(i < n ? get(i) : 0, &total, red);
         if (i < n) out[i] = base + at;
         base += total;
     }
@@ -63,44 +68,63 @@ __device__ __forceinline__ int prefix_of(int n, int* out, int* red, F get) {
     return base;
 }
 
-// Whether `need` pages are free (every thread gets the answer).
-__device__ __forceinline__ bool enough_free(const PageView& p, int need, int* red) {
-    const int words = (p.num_pages + 31) / 32;
-    int have = 0;
-    for (int w0 = 0; w0 < words && have < need; w0 += kPlanThreads) {
-        const int w = w0 + threadIdx.x;
-        unsigned f = w < words ? ~p.taken[w] : 0;
-        if (w == words - 1 && (p.num_pages & 31)) f &= (1u << (p.num_pages & 31)) - 1;
-        int total;
-        block_scan<kPlanThreads>(__popc(f), &total, red);
-        have += total;
-    }
-    return have >= need;
+// The clear bits of word w of the map that are pages.
+__device__ __forceinline__ unsigned free_bits(const PageView& p, int w, unsigned was) {
+    unsigned f = ~was;
+    if (w == p.num_pages >> 5) f &= (1u << (p.num_pages & 31)) - 1;
+    return w < (p.num_pages + 31) / 32 ? f : 0;
+}
+// This thread's word of the map's first NT words: read ahead of everything else, because
+// the pages of an ordinary call come from there.
+template <int NT>
+__device__ __forceinline__ unsigned first_word(const PageView& p) {
+    return (int)threadIdx.x < (p.num_pages + 31) / 32 ? p.taken[threadIdx.x] : ~0u;
 }
 
-// Takes the lowest `need` free pages; give(r, page) places the one of rank r.
-template <typename F>
-__device__ __forceinline__ void take_free(const PageView& p, int need, int* red, F give) {
+// Takes the lowest `need` free pages, or none if there are not as many (false, in every
+// thread); give(r, page) places the one of rank r.  list: room for `need` of them.
+template <int NT, typename F>
+__device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int need, int* red, int* list,
+                                          F give) {
+    if (need == 0) return true;
     const int words = (p.num_pages + 31) / 32;
-    int base = 0;
-    for (int w0 = 0; w0 < words && base < need; w0 += kPlanThreads) {
+    int total, rank = block_scan<NT>(__popc(free_bits(p, threadIdx.x, word0)), &total, red);
+    const int total0 = total;
+    int have = total0;
+    for (int w0 = NT; w0 < words && have < need; w0 += NT) {
         const int w = w0 + threadIdx.x;
-        const unsigned was = w < words ? p.taken[w] : ~0u;
-        unsigned f = ~was;
-        if (w == words - 1 && (p.num_pages & 31)) f &= (1u << (p.num_pages & 31)) - 1;
-        int total, r = base + block_scan<kPlanThreads>(__popc(f), &total, red);
-        unsigned now = was;
-        while (f && r < need) {
+        block_scan<NT>(__popc(free_bits(p, w, w < words ? p.taken[w] : ~0u)), &total, red);
+        have += total;
+    }
+    if (have < need) return false;
+    // A word's owner only lists its pages by rank (the pages of a small call all come from
+    // one or two words, so one or two threads); placing them is every thread's work.
+    auto take = [&](int w, unsigned was, int r) {
+        unsigned f = free_bits(p, w, was), now = was;
+        for (; f && r < need; ++r) {
             const int bit = __ffs(f) - 1;
             f &= f - 1;
             now |= 1u << bit;
-            const int page = w * 32 + bit;
-            p.refs[page] = 1;
-            give(r++, page);
+            list[r] = w * 32 + bit;
         }
         if (now != was) p.taken[w] = now;
+    };
+    take(threadIdx.x, word0, rank);
+    int base = total0;
+    for (int w0 = NT; w0 < words && base < need; w0 += NT) {
+        const int w = w0 + threadIdx.x;
+        const unsigned was = w < words ? p.taken[w] : ~0u;
+        rank = base + block_scan<NT>(__popc(free_bits(p, w, was)), &total, red);
+        take(w, was, rank);
         base += total;
     }
+    __syncthreads();
+    for (int r = threadIdx.x; r < need; r += NT) {
+        const int page = list[r];
+        p.refs[page] = 1;
+        give(r, page);
+    }
+    return true;
 }
 
 __device__ __forceinline__ void drop_ref(const PageView& p, int page) {
@@ -112,13 +136,21 @@ __device__ __forceinline__ bool bad_slot(const PageView& p, unsigned* seen, int 
     if (s < 0 || s >= p.num_seqs) return true;
     return (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31)) & 1;
 }
+template <int NT>
 __device__ __forceinline__ void begin_call(const PageView& p, PlanShared* sh) {
-    for (int w = threadIdx.x; w < (p.num_seqs + 31) / 32; w += kPlanThreads) sh->seen[w] = 0;
+    for (int w = threadIdx.x; w < (p.num_seqs + 31) / 32; w += NT) sh->seen[w] = 0;
     if (threadIdx.x == 0) sh->bad = 0;
     __syncthreads();
 }
 __device__ __forceinline__ void write_header(int* plan, int kind, int n, int items) {
     plan[0] = kind; plan[1] = n; plan[2] = items; plan[3] = 0;
+}
+// The sequence of every page item, so that the kernels that work on items need no search.
+template <int NT>
+__device__ __forceinline__ void write_owners(const PageView& p, int* plan, int n, const int* prefix,
+                                             int items) {
+    int* owner = plan_owner(plan, n, p.max_pages);
+    for (int x = threadIdx.x; x < items; x += NT) owner[x] = owner_of(prefix, n, x);
 }
 
 __global__ __launch_bounds__(256) void pages_reset(PageView p) {
@@ -129,15 +161,23 @@ __global__ __launch_bounds__(256) void pages_reset(PageView p) {
     if (i == 0) *p.status = 0;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void pages_reserve(PageView p, BatchView b, int* plan) {
+template <int NT>
+__global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int* plan) {
     __shared__ PlanShared sh;
     const int n = b.n, G = 1 << p.shift;
+    const unsigned word0 = first_word<NT>(p);
     int* items = plan_array(plan, n, PL_ITEMS);
-    int* first = plan_array(plan, n, PL_FIRST);
-    int* tail = plan_array(plan, n, PL_TAIL);
-    int* rows = plan_array(plan, n, PL_ROWS);
-    begin_call(p, &sh);
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    int* g_first = plan_array(plan, n, PL_FIRST);
+    int* g_tail = plan_array(plan, n, PL_TAIL);
+    int* g_rows = plan_array(plan, n, PL_ROWS);
+    int* g_slot = plan_array(plan, n, PL_SLOT);
+    const bool near = n <= kNear;
+    int* first = near ? sh.near[0] : g_first;
+    int* tail = near ? sh.near[1] : g_tail;
+    int* rows = near ? sh.near[2] : g_rows;
+    int* slot = near ? sh.near[3] : g_slot;
+    begin_call<NT>(p, &sh);
+    for (int i = threadIdx.x; i < n; i += NT) {
         const int s = slot_of(b, i), r = row_count(b, i);
         int bad = 0, len = 0, src = -1;
         if (bad_slot(p, sh.seen, s)) {
@@ -147,66 +187,68 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve(PageView p, BatchV
             if ((long long)len + r > ((long long)p.max_pages << p.shift)) bad = OCCAM_PAGES_TOO_LONG;
             else if (r > 0 && (len & (G - 1))) src = p.table[(size_t)s * p.max_pages + (len >> p.shift)];
         }
-        first[i] = len;
-        tail[i] = src;
-        rows[i] = bad ? 0 : r;
+        first[i] = g_first[i] = len;
+        tail[i] = g_tail[i] = src;
+        rows[i] = g_rows[i] = bad ? 0 : r;
+        slot[i] = g_slot[i] = s;
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
     // The pages wanted: those behind the present last one, and one in the place of a shared
     // partly filled one.
-    const int need = prefix_of(n, sh.need, sh.red, [&](int i) {
+    const int need = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
         const int len = first[i], r = rows[i];
         const int more = ((len + r + G - 1) >> p.shift) - ((len + G - 1) >> p.shift);
         return more + (tail[i] >= 0 && p.refs[tail[i]] > 1);
     });
     __syncthreads();
-    if (!sh.bad && !enough_free(p, need, sh.red)) {
-        if (threadIdx.x == 0) sh.bad = OCCAM_PAGES_FULL;
-        __syncthreads();
-    }
-    if (sh.bad) {
-        for (int i = threadIdx.x; i <= n; i += kPlanThreads) {
+    int* list = need <= kNear ? sh.list : plan_owner(plan, n, p.max_pages);
+    // A shared last page is replaced by the first page its sequence gets: table entry
+    // len / G; otherwise the first one goes behind, at ceil(len / G).
+    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
+            const int i = owner_of(sh.need, n, r), len = first[i];
+            const int wanted = sh.need[i + 1] - sh.need[i];
+            const int pages = (len + rows[i] + G - 1) >> p.shift;
+            const int j = pages - wanted + (r - sh.need[i]);
+            p.table[(size_t)slot[i] * p.max_pages + j] = page;
+        })) {
+        for (int i = threadIdx.x; i <= n; i += NT) {
             items[i] = 0;
-            if (i < n) rows[i] = 0;
+            if (i < n) g_rows[i] = 0;
         }
         if (threadIdx.x == 0) {
-            atomicOr(p.status, sh.bad);
+            atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
             write_header(plan, kPlanReserve, n, 0);
         }
         return;
     }
-    // A shared last page is replaced by the first page its sequence gets: table entry
-    // len / G; otherwise the first one goes behind, at ceil(len / G).
-    take_free(p, need, sh.red, [&](int r, int page) {
-        const int i = owner_of(sh.need, n, r), len = first[i];
-        const int wanted = sh.need[i + 1] - sh.need[i];
-        const int pages = (len + rows[i] + G - 1) >> p.shift;
-        const int j = pages - wanted + (r - sh.need[i]);
-        p.table[(size_t)slot_of(b, i) * p.max_pages + j] = page;
-    });
+    // Only after the taking: a page given up here is not one of those just taken.
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < n; i += NT) {
         if (rows[i] == 0) continue;
-        const int s = slot_of(b, i), len = first[i];
-        // Freed only now: a page given up here is not one of those just taken.
-        if (tail[i] >= 0 && p.table[(size_t)s * p.max_pages + (len >> p.shift)] != tail[i])
-            drop_ref(p, tail[i]);
-        p.length[s] = len + rows[i];
+        p.length[slot[i]] = first[i] + rows[i];
+        // One page more than lies behind: the shared tail was replaced.
+        const int more = ((first[i] + rows[i] + G - 1) >> p.shift) - ((first[i] + G - 1) >> p.shift);
+        if (sh.need[i + 1] - sh.need[i] > more) drop_ref(p, tail[i]);
     }
-    const int total = prefix_of(n, items, sh.red, [&](int i) {
+    __syncthreads();
+    const int total = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
         const int len = first[i], r = rows[i];
         return r > 0 ? ((len + r + G - 1) >> p.shift) - (len >> p.shift) : 0;
     });
+    __syncthreads();
+    for (int i = threadIdx.x; i <= n; i += NT) items[i] = sh.need[i];
+    write_owners<NT>(p, plan, n, sh.need, total);
     if (threadIdx.x == 0) write_header(plan, kPlanReserve, n, total);
 }
 
-__global__ __launch_bounds__(kPlanThreads) void fork_plan(PageView p, int n, const int* src,
-                                                          const int* dst, int* plan) {
+template <int NT>
+__global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* src, const int* dst,
+                                                int* plan) {
     __shared__ PlanShared sh;
     int* lens = plan_array(plan, n, PL_ITEMS);
-    begin_call(p, &sh);
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    begin_call<NT>(p, &sh);
+    for (int i = threadIdx.x; i < n; i += NT) {
         const int s = src[i], t = dst[i];
         int len = 0;
         if (bad_slot(p, sh.seen, t) || s < 0 || s >= p.num_seqs || p.length[t] != 0) sh.bad = 1;
@@ -215,8 +257,8 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(PageView p, int n, con
     }
     __syncthreads();
     if (sh.bad) {
-        for (int i = threadIdx.x; i < n; i += kPlanThreads) lens[i] = -1;
-        if (threadIdx.x == 0) atomicOr(p.status, OCCAM_PAGES_BAD_SEQ);
+        for (int i = threadIdx.x; i < n; i += NT) lens[i] = -1;
+        if (threadIdx.x == 0) atomicOr(p.status, (int)OCCAM_PAGES_BAD_SEQ);
     }
     if (threadIdx.x == 0) write_header(plan, kPlanFork, n, 0);
 }
@@ -251,22 +293,47 @@ __global__ __launch_bounds__(256) void pages_free(PageView p, const int* seq) {
     for (int j = threadIdx.x; j < pages; j += 256) drop_ref(p, row[j]);
 }
 
+// The first of m ascending distinct indices that is not its own position (m if none): the
+// first token dropped.  Seven probes a round, side by side.
+__device__ __forceinline__ int first_gap(const int* idx, int m) {
+    int lo = 0, hi = m;                        // idx[lo - 1] == lo - 1; idx[hi] != hi or hi == m
+    while (hi - lo > 0) {
+        const int step = (hi - lo + 7) >> 3;
+        int at[7], good = 0;
+#pragma unroll
+        for (int k = 0; k < 7; ++k) {
+            const int x = lo + (k + 1) * step - 1;
+            at[k] = x < hi ? idx[x] - x : 1;
+        }
+#pragma unroll
+        for (int k = 0; k < 7; ++k) good += at[k] == 0 && good == k;
+        const int from = lo + good * step;
+        const int to = good < 7 ? lo + (good + 1) * step - 1 : hi;
+        lo = from;
+        hi = to < hi ? to : hi;
+    }
+    return lo;
+}
+
 // Compaction, first part: what every sequence drops and which fresh pages it gets, written
 // into the plan's page lists from the first changed page on.
-__global__ __launch_bounds__(kPlanThreads) void keep_plan(PageView p, int n, const int* seq,
-                                                          const int* start, const int* span,
-                                                          const int* idx, const int* off, int* plan) {
+template <int NT>
+__global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* seq, const int* start,
+                                                const int* span, const int* idx, const int* off,
+                                                int* plan) {
     __shared__ PlanShared sh;
     const int G = 1 << p.shift;
+    const unsigned word0 = first_word<NT>(p);
     int* items = plan_array(plan, n, PL_ITEMS);
-    int* first = plan_array(plan, n, PL_FIRST);
-    int* olds = plan_array(plan, n, PL_OLD);
-    int* news = plan_array(plan, n, PL_NEW);
-    int* starts = plan_array(plan, n, PL_START);
-    int* spans = plan_array(plan, n, PL_SPAN);
-    int* slots = plan_array(plan, n, PL_SLOT);
-    begin_call(p, &sh);
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    int* g_first = plan_array(plan, n, PL_FIRST);
+    int* g_olds = plan_array(plan, n, PL_OLD);
+    int* g_news = plan_array(plan, n, PL_NEW);
+    const bool near = n <= kNear;
+    int* first = near ? sh.near[0] : g_first;
+    int* olds = near ? sh.near[1] : g_olds;
+    int* news = near ? sh.near[2] : g_news;
+    begin_call<NT>(p, &sh);
+    for (int i = threadIdx.x; i < n; i += NT) {
         const int s = seq[i], a = start[i], m = span[i], o = off[i], c = off[i + 1] - o;
         int bad = 0, len = 0, now = 0, f = 0;
         if (bad_slot(p, sh.seen, s)) {
@@ -276,47 +343,44 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan(PageView p, int n, con
             if (a < 0 || m < 0 || (long long)a + m > len || c < 0 || c > m) {
                 bad = OCCAM_PAGES_BAD_SPAN;
             } else if (c < m) {
-                // The first index that is not its own position: the first token dropped.
-                int lo = 0, hi = c;
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (idx[o + mid] == mid) lo = mid + 1; else hi = mid;
-                }
                 now = len - m + c;
-                f = (a + lo) >> p.shift;
+                f = (a + first_gap(idx + o, c)) >> p.shift;
             } else {
                 f = (len + G - 1) >> p.shift;            // nothing dropped
             }
         }
-        olds[i] = len; news[i] = now; first[i] = f; starts[i] = a; spans[i] = m; slots[i] = s;
+        first[i] = g_first[i] = f;
+        olds[i] = g_olds[i] = len;
+        news[i] = g_news[i] = now;
+        plan_array(plan, n, PL_START)[i] = a;
+        plan_array(plan, n, PL_SPAN)[i] = m;
+        plan_array(plan, n, PL_SLOT)[i] = s;
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
-    const int need = prefix_of(n, sh.need, sh.red, [&](int i) {
+    const int need = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
         const int pages = ((news[i] + G - 1) >> p.shift) - first[i];
         return sh.bad || pages < 0 ? 0 : pages;
     });
     __syncthreads();
-    if (!sh.bad && !enough_free(p, need, sh.red)) {
-        if (threadIdx.x == 0) sh.bad = OCCAM_PAGES_FULL;
-        __syncthreads();
-    }
-    if (sh.bad) {
-        for (int i = threadIdx.x; i <= n; i += kPlanThreads) {
+    int* list = need <= kNear ? sh.list : plan_owner(plan, n, p.max_pages);
+    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
+            const int i = owner_of(sh.need, n, r);
+            plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
+        })) {
+        for (int i = threadIdx.x; i <= n; i += NT) {
             items[i] = 0;
-            if (i < n) { news[i] = olds[i]; first[i] = (olds[i] + G - 1) >> p.shift; }
+            if (i < n) { g_news[i] = olds[i]; g_first[i] = (olds[i] + G - 1) >> p.shift; }
         }
         if (threadIdx.x == 0) {
-            atomicOr(p.status, sh.bad);
+            atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
             write_header(plan, kPlanKeep, n, 0);
         }
         return;
     }
-    take_free(p, need, sh.red, [&](int r, int page) {
-        const int i = owner_of(sh.need, n, r);
-        plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
-    });
-    for (int i = threadIdx.x; i <= n; i += kPlanThreads) items[i] = sh.need[i];
+    for (int i = threadIdx.x; i <= n; i += NT) items[i] = sh.need[i];
+    __syncthreads();                       // the list may lie where the owners go
+    write_owners<NT>(p, plan, n, sh.need, need);
     if (threadIdx.x == 0) write_header(plan, kPlanKeep, n, need);
 }
 
@@ -347,12 +411,14 @@ hipError_t launch_pages_reset(const PageView& p, hipStream_t s) {
 }
 
 hipError_t launch_pages_reserve(const PageView& p, const BatchView& b, int* plan, hipStream_t s) {
-    return launch(pages_reserve, dim3(1), dim3(kPlanThreads), 0, s, p, b, plan);
+    return b.n <= 256 ? launch(pages_reserve<256>, dim3(1), dim3(256), 0, s, p, b, plan)
+                      : launch(pages_reserve<1024>, dim3(1), dim3(1024), 0, s, p, b, plan);
 }
 
 hipError_t launch_pages_fork(const PageView& p, int n, const int* src, const int* dst, int* plan,
                              hipStream_t s) {
-    hipError_t e = launch(fork_plan, dim3(1), dim3(kPlanThreads), 0, s, p, n, src, dst, plan);
+    hipError_t e = n <= 256 ? launch(fork_plan<256>, dim3(1), dim3(256), 0, s, p, n, src, dst, plan)
+                            : launch(fork_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, src, dst, plan);
     if (e != hipSuccess) return e;
     return launch(fork_copy, dim3(n), dim3(256), 0, s, p, n, src, dst, plan);
 }
@@ -364,8 +430,10 @@ hipError_t launch_pages_free(const PageView& p, int n, const int* seq, hipStream
 hipError_t launch_pages_keep(const PageView& p, int n, const int* seq, const int* start,
                              const int* span, const int* idx, const int* off, int* plan,
                              hipStream_t s) {
-    hipError_t e = launch(keep_plan, dim3(1), dim3(kPlanThreads), 0, s, p, n, seq, start, span, idx,
-                          off, plan);
+    hipError_t e = n <= 256 ? launch(keep_plan<256>, dim3(1), dim3(256), 0, s, p, n, seq, start, span,
+                                     idx, off, plan)
+                            : launch(keep_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, seq, start, span,
+                                     idx, off, plan);
     if (e != hipSuccess) return e;
     return launch(keep_swap, dim3(n), dim3(256), 0, s, p, n, seq, plan);
 }
