@@ -72,7 +72,7 @@ occam_status batch_from(const PageView& p, const occam_batch* b, BatchView* out)
 
 occam_status check_plan(const PageView& p, int n, const void* plan, size_t bytes) {
     if (n < 1 || n > OCCAM_MAX_BATCH) return OCCAM_ERR_INVALID_ARG;
-    if (bytes < plan_ints(n, p.max_pages) * 4) return OCCAM_ERR_WORKSPACE;
+    if (bytes < plan_ints(n, p.max_pages, p.num_pages) * 4) return OCCAM_ERR_WORKSPACE;
     return given(plan, 4) ? OCCAM_OK : OCCAM_ERR_INVALID_ARG;
 }
 
@@ -84,7 +84,7 @@ bool rows_ok(const void* x, long long stride, const CacheView& c, int dtype) {
 
 struct AttendPlan {
     AttendArgs a;
-    size_t off_l, total;
+    size_t off_l, off_cuts, total;
 };
 
 occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView& b,
@@ -103,14 +103,22 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     a.scale2 = scale * kLog2e;
     const long long cap = (long long)p.max_pages << p.shift;
     const long long most = at->max_tokens && at->max_tokens < cap ? at->max_tokens : cap;
-    attend_splits(c, b, a.H, most, &a.chunk, &a.splits);
-    const long long rows = (long long)b.n * b.max_rows;
-    // (row, head) pairs, and workgroups, are numbered in 32 bits.
-    if (rows * a.H >= (1LL << 31) || rows * a.H * a.splits >= (1LL << 33)) return OCCAM_ERR_UNSUPPORTED;
-    if ((long long)b.max_rows * a.g * a.splits * c.Hkv * b.n >= (1LL << 31)) return OCCAM_ERR_UNSUPPORTED;
-    if (a.splits > 1) {
-        out->off_l = align_up((size_t)rows * a.H * a.splits * c.d * sizeof(float));
-        out->total = align_up(out->off_l + (size_t)rows * a.H * a.splits * sizeof(float));
+    // (row, head) pairs are numbered in 32 bits, and so are row blocks.
+    if ((long long)b.n * b.max_rows * a.H >= (1LL << 31) || c.Hkv > 65535) return OCCAM_ERR_UNSUPPORTED;
+    // Units of at least 64 keys of all row blocks (of at least 16 rows), at the longest.
+    if ((double)b.n * ((double)b.max_rows * a.g / 16 + 1) * ((double)cap / 64 + 1) >= 2147483648.0)
+        return OCCAM_ERR_UNSUPPORTED;
+    a.ranges = attend_ranges(c, b, a.H, most);
+    long long slots, cuts;
+    attend_slots(c, b, a.H, a.ranges, &slots, &cuts);
+    if (cuts > 65535) return OCCAM_ERR_UNSUPPORTED;        // a launch's grid.y
+    a.slots = (int)slots;
+    a.num_cuts = (int)cuts;
+    if (slots > 0) {
+        const size_t rows = (size_t)c.Hkv * slots * attend_block_rows(c, b, a.H);
+        out->off_l = align_up(rows * c.dp * sizeof(float));
+        out->off_cuts = align_up(out->off_l + rows * sizeof(float));
+        out->total = align_up(out->off_cuts + (size_t)cuts * sizeof(int4));
     }
     if (out->total < kAlign) out->total = kAlign;
     return OCCAM_OK;
@@ -217,7 +225,7 @@ occam_status occam_rotate(const occam_rotary* rotary, int32_t rows, const int32_
 size_t occam_pages_plan_size(const occam_pages* pages, int32_t n) {
     PageView p;
     if (pages_from(pages, false, &p) != OCCAM_OK || n < 1 || n > OCCAM_MAX_BATCH) return 0;
-    return plan_ints(n, p.max_pages) * 4;
+    return plan_ints(n, p.max_pages, p.num_pages) * 4;
 }
 
 size_t occam_cache_storage_size(const occam_pages* pages, int32_t num_kv_heads, int32_t head_dim) {
@@ -377,6 +385,7 @@ occam_status occam_cache_attend(const occam_pages* pages, const occam_cache* cac
     a.lse = row_lse;
     a.part_o = static_cast<float*>(workspace);
     a.part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + ap.off_l);
+    a.cuts = reinterpret_cast<int4*>(static_cast<char*>(workspace) + ap.off_cuts);
     return hip_ok(launch_cache_attend(a, stream));
 }
 

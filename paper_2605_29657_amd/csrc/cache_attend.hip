@@ -57,11 +57,131 @@ __device__ __forceinline__ f16x2 round_f16(float a, float b) {     // to nearest
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // ---------------------------------------------------------------------------------------
-// Few rows: 16 rows of one key head per workgroup, the keys of one split dealt to its four
+// Division of work.  Per key head there is a row block of so many rows of every sequence,
+// and of each as many units of keys as its rows see.  Lengths are known on the device only.
+// A row block's keys may be cut into parts; each leaves its output and normaliser in a slot
+// of the workspace, and attend_join puts a block's parts together.
+// ---------------------------------------------------------------------------------------
+struct Block {                     // one row block of one sequence
+    int i, T, len, slot, r0, end;  // end: keys its rows see (0 or less: none)
+};
+// Later row blocks of every sequence come first: under a causal mask they are the long ones.
+__device__ __forceinline__ Block block_of(const AttendArgs& a, int entry, int blocks, int rows) {
+    Block t;
+    const int rb = entry / a.b.n;
+    t.i = entry - rb * a.b.n;
+    t.r0 = (blocks - 1 - rb) * rows;
+    t.T = row_count(a.b, t.i);
+    t.slot = slot_of(a.b, t.i);
+    const bool known = t.slot >= 0 && t.slot < a.pg.num_seqs;
+    t.len = known ? a.pg.length[t.slot] : 0;
+    t.slot = known ? t.slot : 0;
+    const int last = (t.r0 + rows - 1) / a.g;
+    t.end = a.causal ? t.len - t.T + (last < t.T - 1 ? last : t.T - 1) + 1 : t.len;
+    return t;
+}
+// Units of keys of a row block: one where there is nothing to see (zeros are written), none
+// where there are no rows.
+__device__ __forceinline__ int units_of(const AttendArgs& a, const Block& t, int unit) {
+    return t.r0 >= t.T * a.g ? 0 : t.end > 0 ? (t.end + unit - 1) / unit : 1;
+}
+
+// The few-row form lays the row blocks end to end and cuts the whole into equal ranges, one
+// per workgroup, as many as the chip holds at once.  Every workgroup sums the lengths up for
+// itself.  A range has at most two parts: of the block it goes on with (slot 0) and of the
+// one it leaves unfinished (slot 1).
+struct Range {
+    int start, stop;               // in units
+    int entry, first;              // the row block that holds `start`, and its first unit
+    int each;                      // units per range
+    Block block;                   // that row block
+};
+// Range `w` of a.ranges over the row blocks of the batch; all NT threads call it.  `red`:
+// NT / 64 + 8 ints of LDS.
+template <int NT>
+__device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks, int rows, int unit,
+                                          int least, int* red) {
+    const int entries = a.b.n * blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int total = 0, base = 0, mine = 0, before = 0;
+    Block block = {};
+    // Exclusive prefix of the units of entries c .. c + NT - 1, and their sum.
+    auto scan = [&](int c) {
+        const int e = c + (int)threadIdx.x;
+        mine = 0;
+        if (e < entries) {
+            block = block_of(a, e, blocks, rows);
+            mine = units_of(a, block, unit);
+        }
+        int s = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(s, o);
+            if (lane >= o) s += y;
+        }
+        __syncthreads();
+        if (lane == 63) red[wave] = s;
+        __syncthreads();
+        int sum = 0;
+        before = s - mine;
+#pragma unroll
+        for (int x = 0; x < NT / 64; ++x) {
+            const int y = red[x];
+            before += x < wave ? y : 0;
+            sum += y;
+        }
+        return sum;
+    };
+    for (int c = 0; c < entries; c += NT) total += scan(c);
+    Range r;
+    r.each = (total + a.ranges - 1) / a.ranges;
+    r.each = r.each < least ? least : r.each;
+    // (Products past 2^31 would be past the end: ranges * each < total + ranges * least.)
+    r.start = w * r.each;
+    r.stop = r.start + r.each < total ? r.start + r.each : total;
+    r.entry = r.first = 0;
+    if (r.start >= total) return r;
+    for (int c = 0; c < entries; c += NT) {
+        const int sum = entries <= NT ? total : scan(c);
+        if (r.start < base + sum) {
+            const int at = base + before;
+            if (at <= r.start && r.start < at + mine) {
+                int* out = red + NT / 64;
+                out[0] = c + (int)threadIdx.x; out[1] = at;
+                out[2] = block.i; out[3] = block.T; out[4] = block.len;
+                out[5] = block.slot; out[6] = block.r0; out[7] = block.end;
+            }
+            __syncthreads();
+            const int* out = red + NT / 64;
+            r.entry = uniform(out[0]);
+            r.first = uniform(out[1]);
+            r.block = Block{uniform(out[2]), uniform(out[3]), uniform(out[4]),
+                            uniform(out[5]), uniform(out[6]), uniform(out[7])};
+            break;
+        }
+        base += sum;
+    }
+    return r;
+}
+// Tells attend_join of the row block that the range's start cuts, where this is the block's
+// first cut: {entry, parts, first slot, slots from a part to the next}; {-1} otherwise.
+// Written for every range, the empty ones behind the end of the work among them:
+// attend_join reads them all.
+__device__ __forceinline__ void note_cut(const AttendArgs& a, const Range& r, int w, int unit) {
+    int4 cut = {-1, 0, 0, 0};
+    if (r.start < r.stop && r.first < r.start && r.first >= r.start - r.each) {
+        const int end = r.first + units_of(a, r.block, unit);
+        cut = int4{r.entry, (end - 1) / r.each - w + 2, 2 * (w - 1) + 1, 2};
+    }
+    a.cuts[w] = cut;
+}
+
+// ---------------------------------------------------------------------------------------
+// Few rows: 16 rows of one key head at a time, their keys dealt to the workgroup's four
 // waves in steps of 32, joined in LDS.  Bound by reading the codes once: a wave has the
 // loads of two steps in flight (8 KB each at d = 128) and several workgroups share a CU.
 // ---------------------------------------------------------------------------------------
 constexpr int kStep = 32, kFewWaves = 4, kFewRows = 16;
+constexpr int kFewUnit = kStep * kFewWaves;
 
 // Page numbers and scales of the 64 16-token groups around a wave's position, one per lane.
 struct Window {
@@ -70,34 +190,32 @@ struct Window {
 };
 
 template <int DP>
-__global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) void attend_few(AttendArgs a) {
     constexpr int NC = DP / 64;            // 64-element chunks of a row
     __shared__ float jo[kFewWaves][kFewRows][64 + 4];
     __shared__ float jm[kFewWaves][kFewRows], jl[kFewWaves][kFewRows];
+    __shared__ int red[kFewWaves + 8];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 15, g4 = lane >> 4;
-    // blockIdx.x: (row block, split, key head, sequence), the last slowest.
-    int w = blockIdx.x;
-    const int blocks = (((a.b.off ? a.b.max_rows : a.b.rows) * a.g) + kFewRows - 1) / kFewRows;
-    const int rb = w % blocks; w /= blocks;
-    const int sp = w % a.splits; w /= a.splits;
-    const int h = w % a.c.Hkv, i = w / a.c.Hkv;
-    const int T = row_count(a.b, i), slot = slot_of(a.b, i);
-    const int r0 = rb * kFewRows;
-    if (r0 >= T * a.g) return;
-    const bool known = slot >= 0 && slot < a.pg.num_seqs;
-    const int len = known ? a.pg.length[slot] : 0;
+    const int w = blockIdx.x / a.c.Hkv, h = blockIdx.x - w * a.c.Hkv;
+    const int blocks = (a.b.max_rows * a.g + kFewRows - 1) / kFewRows;
+    const Range range = range_of<64 * kFewWaves>(a, w, blocks, kFewRows, kFewUnit, 1, red);
+    if (a.slots > 0 && h == 0 && threadIdx.x == 0) note_cut(a, range, w, kFewUnit);
+    int entry = range.entry, at_unit = range.start - range.first;
+    for (int now = range.start; now < range.stop && entry < a.b.n * blocks; ++entry, at_unit = 0) {
+    const Block block = entry == range.entry ? range.block : block_of(a, entry, blocks, kFewRows);
+    const int units = units_of(a, block, kFewUnit);
+    if (units == 0) continue;
+    const int take = units - at_unit < range.stop - now ? units - at_unit : range.stop - now;
+    const bool whole = take == units;
+    now += take;
+    const int i = block.i, T = block.T, len = block.len, r0 = block.r0;
     const int row = r0 + n, t = row / a.g, hh = h * a.g + row - t * a.g;
     const bool live = t < T;
     const int last = live ? (a.causal ? len - T + t : len - 1) : -1;       // last key seen
-    const int tmax = (r0 + kFewRows - 1) / a.g < T - 1 ? (r0 + kFewRows - 1) / a.g : T - 1;
-    const int end = a.causal ? len - T + tmax + 1 : len;                   // keys of the block
-    // The split's keys; the last split of the launch takes all that is left.
-    const int lo = sp * a.chunk;
-    int hi = sp == a.splits - 1 ? end : lo + a.chunk;
-    hi = hi < end ? hi : end;
-    if (sp > 0 && lo >= end) return;
-    const int* table = a.pg.table + (size_t)(known ? slot : 0) * a.pg.max_pages;
+    const int lo = at_unit * kFewUnit;
+    const int hi = lo + take * kFewUnit < block.end ? lo + take * kFewUnit : block.end;
+    const int* table = a.pg.table + (size_t)block.slot * a.pg.max_pages;
 
     // Queries: reduction slots as the keys' 16-byte loads number them.
     bf16x8 q[NC][2];
@@ -141,8 +259,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
             // A group past the end reads the one before it again; its keys are masked.
             const int at = gr + u < groups ? gr + u : groups - 1, src = at & 63;
             const int page = __builtin_amdgcn_readlane(win.page, src);
-            x.ks[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(win.ks), src));
-            x.vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(win.vs), src));
             const int tok = (at << 4) & ((1 << a.pg.shift) - 1);
             const size_t off = ((size_t)page * a.c.Hkv + h) * a.c.block + (size_t)tok * DP;
             const unsigned char* kp = a.c.k + off + n * DP + g4 * 16;
@@ -152,6 +268,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
                 x.k[u][c] = *reinterpret_cast<const u32x4*>(kp + c * 64);
                 x.v[u][c] = *reinterpret_cast<const u32x4*>(vp + c * 256);
             }
+        }
+        // The scales after the codes, which need only the page numbers of a new window.
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int src = (gr + u < groups ? gr + u : groups - 1) & 63;
+            x.ks[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(win.ks), src));
+            x.vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(win.vs), src));
         }
     };
     auto compute = [&](int pos, Codes& x) {
@@ -243,6 +366,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     constexpr float kDrop = 0x1p-14f;                       // undoes kLift
+    __syncthreads();                                        // read for the row block before
     if (g4 == 0) { jm[wave][n] = m; jl[wave][n] = l * kDrop; }
     __syncthreads();
     // 16 threads per row, four elements each of every 64-element chunk.
@@ -261,7 +385,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
     const float lse2 = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;   // base 2
     const float unref = exp_scale(ref - (int)kLift);
     const long long orow = (long long)row_begin(a.b, i) + rt;
-    const size_t at = ((size_t)orow * a.H + rh) * a.splits + sp;
+    const size_t at = ((size_t)h * a.slots + 2 * w + (lo > 0 ? 0 : 1)) * kFewRows + r;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         if (c) __syncthreads();
@@ -277,7 +401,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
         for (int x = 0; x < kFewWaves; ++x)
             y += wgt[x] * *reinterpret_cast<const f32x4*>(&jo[x][r][part * 4]);
         y *= inv;
-        if (a.splits == 1) {
+        if (whole) {
             ushort4 o;
             o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
             o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
@@ -285,12 +409,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
             o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
             *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)rh * a.c.d + e0) = o;
         } else {
-            *reinterpret_cast<f32x4*>(a.part_o + at * a.c.d + e0) = y;
+            *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = y;
         }
     }
     if (part == 0 && rt < T) {
-        if (a.splits == 1) { if (a.lse) a.lse[orow * a.H + rh] = lse2 * kLn2; }
+        if (whole) { if (a.lse) a.lse[orow * a.H + rh] = lse2 * kLn2; }
         else a.part_l[at] = lse2;
+    }
     }
 }
 
@@ -312,6 +437,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void attend_few(AttendArgs a) {
 // buffers.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
+constexpr int kManyLeast = 4;              // tiles per part at least
 constexpr float kManyLift = 6.f, kManySlack = 8.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -352,32 +478,31 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     constexpr int HALF = kTile * DP * 2;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 31, half = lane >> 5;
-    // Later row blocks of every sequence first: under a causal mask they are the long ones.
-    const int blocks = (((a.b.off ? a.b.max_rows : a.b.rows) * a.g) + ROWS - 1) / ROWS;
-    const int tasks = a.splits * a.c.Hkv * a.b.n;
-    int w = blockIdx.x;
-    const int rb = blocks - 1 - w / tasks; w %= tasks;
-    const int sp = w % a.splits; w /= a.splits;
-    const int h = w % a.c.Hkv, i = w / a.c.Hkv;
-    const int T = row_count(a.b, i), slot = slot_of(a.b, i);
-    const int r0 = rb * ROWS;
-    if (r0 >= T * a.g) return;
-    const bool known = slot >= 0 && slot < a.pg.num_seqs;
-    const int len = known ? a.pg.length[slot] : 0;
+    // A workgroup per part of a row block; every sequence's last row block first.
+    const int blocks = (a.b.max_rows * a.g + ROWS - 1) / ROWS;
+    const int task = blockIdx.x / a.c.Hkv, h = blockIdx.x - task * a.c.Hkv;
+    const int entry = task / a.ranges, part = task - entry * a.ranges;
+    const Block block = block_of(a, entry, blocks, ROWS);
+    const int units = units_of(a, block, kTile);
+    int parts = (units + kManyLeast - 1) / kManyLeast;
+    parts = parts < a.ranges ? parts : a.ranges;
+    if (a.slots > 0 && h == 0 && part == 0 && threadIdx.x == 0)
+        a.cuts[entry] = int4{parts > 1 ? entry : -1, parts, entry * a.ranges, 1};
+    if (part >= parts) return;
+    const bool whole = parts == 1;
+    const int i = block.i, T = block.T, len = block.len, r0 = block.r0;
+    const int lo = (int)((long long)units * part / parts) * kTile;
+    const int up = (int)((long long)units * (part + 1) / parts) * kTile;
+    const int hi = up < block.end ? up : block.end;
     auto block_end = [&](int first, int rows) {              // keys that these rows see
         if (first >= T * a.g) return 0;
         if (!a.causal) return len;
         const int t = (first + rows - 1) / a.g;
         return len - T + (t < T - 1 ? t : T - 1) + 1;
     };
-    const int end = block_end(r0, ROWS);
-    const int lo = sp * a.chunk;
-    int hi = sp == a.splits - 1 ? end : lo + a.chunk;
-    hi = hi < end ? hi : end;
-    if (sp > 0 && lo >= end) return;
     const int mine = uniform(block_end(r0 + wave * 32, 32));
     const int wave_hi = mine < hi ? mine : hi;
-    const int* table = a.pg.table + (size_t)(known ? slot : 0) * a.pg.max_pages;
+    const int* table = a.pg.table + (size_t)block.slot * a.pg.max_pages;
     const int row = r0 + wave * 32 + n, t = row / a.g, hh = h * a.g + row - t * a.g;
     const bool live = t < T;
     const int last = live ? (a.causal ? len - T + t : len - 1) : -1;
@@ -655,109 +780,90 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     l += __shfl_xor(l, 32);
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) - kManyLift : -INFINITY;
-    if (!live) return;
     const float f = exp_scale(ref);
     const long long orow = (long long)row_begin(a.b, i) + t;
-    const size_t at = ((size_t)orow * a.H + hh) * a.splits + sp;
+    const size_t at = ((size_t)h * a.slots + task) * ROWS + wave * 32 + n;
     unsigned short* out = a.out + orow * a.out_stride + (long long)hh * a.c.d;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
             const int e0 = d * 32 + 8 * e4 + 4 * half;
-            if (e0 >= a.c.d) continue;
+            if (!live || e0 >= a.c.d) continue;
             float y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = acc[d][e4 * 4 + e] * inv * f;
-            if (a.splits == 1) {
+            if (whole) {
                 union { bf16x2 p[2]; u32x2 v; } o;
                 o.p[0] = bf16x2{(__bf16)y[0], (__bf16)y[1]};
                 o.p[1] = bf16x2{(__bf16)y[2], (__bf16)y[3]};
                 *reinterpret_cast<u32x2*>(out + e0) = o.v;
             } else {
-                *reinterpret_cast<f32x4*>(a.part_o + at * a.c.d + e0) = f32x4{y[0], y[1], y[2], y[3]};
+                *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = f32x4{y[0], y[1], y[2], y[3]};
             }
         }
-    if (half == 0) {
-        if (a.splits == 1) { if (a.lse) a.lse[orow * a.H + hh] = lse2 * kLn2; }
+    if (live && half == 0) {
+        if (whole) { if (a.lse) a.lse[orow * a.H + hh] = lse2 * kLn2; }
         else a.part_l[at] = lse2;
     }
 }
 
-// Joins the splits of a row and head: weights 2^(lse - max), each split's output already
-// divided by its own sum.  A workgroup per (row, head): the splits are dealt to 1024 / DP
-// groups of threads, four elements a thread, so that a lone request's many splits are read
-// side by side.
+// Joins the parts of the row blocks that were cut: weights 2^(lse - max), each part's output
+// already divided by its own sum.  blockIdx.y: a place in the list of cut blocks; z: key
+// head; x: groups of 1024 / DP rows of the block, four elements a thread.
 template <int DP>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows) {
-    constexpr int TE = DP / 4, NG = 256 / TE;
-    __shared__ f32x4 jo[NG][TE];
-    __shared__ float js[NG];
-    const int lane = threadIdx.x & 63;
-    const int maxr = a.b.off ? a.b.max_rows : a.b.rows, per = maxr * a.H;
-    const int i = blockIdx.x / per, x = blockIdx.x - i * per, t = x / a.H, hh = x - t * a.H;
-    const int T = row_count(a.b, i), slot = slot_of(a.b, i);
-    if (t >= T) return;
-    const int len = slot >= 0 && slot < a.pg.num_seqs ? a.pg.length[slot] : 0;
-    const long long orow = (long long)row_begin(a.b, i) + t;
-    const size_t at = ((size_t)orow * a.H + hh) * a.splits;
-    const int te = threadIdx.x % TE, grp = threadIdx.x / TE;
-    const bool in = te * 4 < a.c.d;
-    // The first splits of every group are read before anything is known of the
-    // sequence (what a split that does not exist left there is not used).
-    constexpr int AHEAD = 4;
-    float pl[AHEAD], l0 = -INFINITY;
-    f32x4 po[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-        const int p = grp + k * NG;
-        pl[k] = p < a.splits ? a.part_l[at + p] : -INFINITY;
-        po[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (in && p < a.splits) po[k] = *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
-    }
-    if (lane < a.splits) l0 = a.part_l[at + lane];
-    // The keys of the row block that the row was computed in decide which splits exist.
-    const int r = t * a.g + hh % a.g, r1 = (r / block_rows + 1) * block_rows - 1;
-    const int tm = r1 / a.g < T - 1 ? r1 / a.g : T - 1;
-    const int end = a.causal ? len - T + tm + 1 : len;
-    int parts = end > 0 ? (end + a.chunk - 1) / a.chunk : 1;
-    parts = parts < a.splits ? parts : a.splits;
-    float top = lane < parts ? l0 : -INFINITY;
-    for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, a.part_l[at + p]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float base = top == -INFINITY ? 0.f : top;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    auto add = [&](int p, float pl, f32x4 po) {
-        if (p >= parts) return;
-        const float wgt = __builtin_amdgcn_exp2f(pl - base);
-        sum += wgt;
-        y += wgt * po;
+    constexpr int TE = DP / 4, NR = 256 / TE;
+    const int h = blockIdx.z;
+    const int4 cut = a.cuts[blockIdx.y];
+    if (cut.x < 0) return;
+    const int blocks = (a.b.max_rows * a.g + block_rows - 1) / block_rows;
+    const Block b = block_of(a, cut.x, blocks, block_rows);
+    const int te = threadIdx.x % TE, rr = blockIdx.x * NR + threadIdx.x / TE;
+    const int i = b.i, row = b.r0 + rr, t = row / a.g, hh = h * a.g + row - t * a.g;
+    if (t >= b.T || te * 4 >= a.c.d) return;
+    const int parts = cut.y;
+    auto at = [&](int p) {
+        const int slot = cut.z + (p ? p * cut.w - (cut.w - 1) : 0);
+        return ((size_t)h * a.slots + slot) * block_rows + rr;
     };
+    float top = -INFINITY, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;                       // parts read side by side
+#pragma unroll 1
+    for (int p0 = 0; p0 < parts; p0 += U) {
+        float l[U], most = top;
+        f32x4 o[U];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) add(grp + k * NG, pl[k], po[k]);
-#pragma unroll 4
-    for (int p = grp + AHEAD * NG; p < parts; p += NG) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (in) x = *reinterpret_cast<const f32x4*>(a.part_o + (at + p) * a.c.d + te * 4);
-        add(p, a.part_l[at + p], x);
+        for (int u = 0; u < U; ++u) {
+            l[u] = -INFINITY;
+            o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (p0 + u >= parts) continue;
+            l[u] = a.part_l[at(p0 + u)];
+            o[u] = *reinterpret_cast<const f32x4*>(a.part_o + at(p0 + u) * DP + te * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) most = fmaxf(most, l[u]);
+        if (most == -INFINITY) continue;
+        const float fade = __builtin_amdgcn_exp2f(top - most);
+        sum *= fade;
+        y *= fade;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float wgt = __builtin_amdgcn_exp2f(l[u] - most);
+            sum += wgt;
+            y += wgt * o[u];
+        }
+        top = most;
     }
-    jo[grp][te] = y;
-    if (te == 0) js[grp] = sum;
-    __syncthreads();
-    if (grp) return;
-#pragma unroll
-    for (int g = 1; g < NG; ++g) { y += jo[g][te]; sum += js[g]; }
+    const long long orow = (long long)row_begin(a.b, i) + t;
     y *= sum > 0.f ? 1.f / sum : 0.f;
-    if (in) {
-        ushort4 o;
-        o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
-        o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
-        o.z = __builtin_bit_cast(unsigned short, (__bf16)y[2]);
-        o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
-        *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)hh * a.c.d + te * 4) = o;
-    }
+    ushort4 o;
+    o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
+    o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
+    o.z = __builtin_bit_cast(unsigned short, (__bf16)y[2]);
+    o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
+    *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)hh * a.c.d + te * 4) = o;
     if (te == 0 && a.lse)
         a.lse[orow * a.H + hh] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
@@ -766,38 +872,51 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows)
 
 // Which form: more rows than two blocks of the few-row form go to the many-row form.
 int attend_block_rows(const CacheView& c, const BatchView& b, int H) {
-    const long long rows = (long long)(b.off ? b.max_rows : b.rows) * (H / c.Hkv);
+    const long long rows = (long long)b.max_rows * (H / c.Hkv);
     return rows <= 2 * kFewRows ? kFewRows : c.dp == 128 ? 256 : 128;
 }
 
-// Keys per split and splits: enough workgroups to fill the chip several times over, at
-// least 128 keys each.
-void attend_splits(const CacheView& c, const BatchView& b, int H, long long max_tokens, int* chunk,
-                   int* splits) {
+static long long attend_blocks(const CacheView& c, const BatchView& b, int H) {
     const int br = attend_block_rows(c, b, H);
-    const long long rows = (long long)(b.off ? b.max_rows : b.rows) * (H / c.Hkv);
-    const long long tasks = (long long)b.n * c.Hkv * ((rows + br - 1) / br);
-    const long long least = 128;
-    long long want = (br == kFewRows ? 2048 : 512) / tasks;
-    const long long most = (max_tokens + least - 1) / least;
-    want = want < 1 ? 1 : want > most ? most : want;
-    want = want < 1 ? 1 : want;
-    long long per = (max_tokens + want - 1) / want;
-    per = (per + kTile - 1) / kTile * kTile;
-    per = per < least ? least : per;
-    *chunk = (int)per;
-    *splits = (int)((max_tokens + per - 1) / per);
-    if (*splits < 1) *splits = 1;
+    return ((long long)b.max_rows * (H / c.Hkv) + br - 1) / br;
+}
+
+// Few rows: ranges per key head, the workgroups that are resident at once (registers: 4, 3
+// and 1 per CU at dp = 64, 128 and 256), no more than there is work at the longest.
+// Many rows: the most parts of a row block, enough for two workgroups per CU, of at least
+// kManyLeast tiles each.
+int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
+    const long long blocks = b.n * attend_blocks(c, b, H);
+    long long want, most;
+    if (attend_block_rows(c, b, H) == kFewRows) {
+        want = 256 * (c.dp == 64 ? 4 : c.dp == 128 ? 3 : 1) / c.Hkv;
+        most = blocks * ((max_tokens + kFewUnit - 1) / kFewUnit);
+    } else {
+        want = 512 / (blocks * c.Hkv);
+        most = (max_tokens + kTile * kManyLeast - 1) / (kTile * kManyLeast);
+    }
+    want = want > most ? most : want;
+    return want < 1 ? 1 : (int)want;
+}
+
+// Slots for parts per key head, and places in the list of cut blocks: none where nothing
+// can be cut.
+void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
+                  long long* cuts) {
+    const long long blocks = b.n * attend_blocks(c, b, H);
+    const bool few = attend_block_rows(c, b, H) == kFewRows;
+    *slots = ranges == 1 ? 0 : few ? 2 * ranges : blocks * ranges;
+    *cuts = ranges == 1 ? 0 : few ? ranges : blocks;
 }
 
 template <int DP>
 static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
     const int br = attend_block_rows(a.c, a.b, a.H);
-    const long long maxr = a.b.off ? a.b.max_rows : a.b.rows;
-    const long long blocks = (maxr * a.g + br - 1) / br;
-    const dim3 grid((unsigned)(blocks * a.splits * a.c.Hkv * a.b.n));
+    const bool few = br == kFewRows;
+    const long long tasks = few ? a.ranges : a.b.n * attend_blocks(a.c, a.b, a.H) * a.ranges;
+    const dim3 grid((unsigned)(tasks * a.c.Hkv));
     hipError_t e;
-    if (br == kFewRows) {
+    if (few) {
         e = launch(attend_few<DP>, grid, dim3(64 * kFewWaves), 0, s, a);
     } else {
         static_assert(32 * many_waves<DP>() == (DP == 128 ? 256 : 128), "rows of a block");
@@ -807,8 +926,8 @@ static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
                            : allow_lds(reinterpret_cast<const void*>(attend_many<DP>), bytes, done);
         if (e == hipSuccess) e = launch(attend_many<DP>, grid, dim3(64 * many_waves<DP>()), bytes, s, a);
     }
-    if (e != hipSuccess || a.splits == 1) return e;
-    return launch(attend_join<DP>, dim3((unsigned)(a.b.n * maxr * a.H)), dim3(256), 0, s, a, br);
+    if (e != hipSuccess || a.slots == 0) return e;
+    return launch(attend_join<DP>, dim3(br / (1024 / DP), a.num_cuts, a.c.Hkv), dim3(256), 0, s, a, br);
 }
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {

@@ -42,19 +42,31 @@ __device__ __forceinline__ int row_count(const BatchView& b, int i) {
 }
 
 // The plan: a header of four ints (kind, n, page items, 0), arrays of n + 1 ints, for keep
-// a page list of max_pages ints per sequence, and the sequence of every page item.
-//   reserve: ITEMS prefix of the pages that receive rows, FIRST tokens held before,
-//            TAIL page that holds the partly filled last page's tokens (or -1), ROWS, SLOT
-//   keep:    ITEMS prefix of the pages rewritten, FIRST page rewritten, OLD tokens before,
-//            NEW tokens after, START and SPAN of the span, SLOT
-//   fork:    ITEMS tokens of the source, or -1 where the call failed
+// a page list of max_pages ints per sequence, and a record of eight ints for every page item
+// (a page that receives rows, or that is rewritten): what the kernels that work on items
+// need to know, found with one load.
+//   keep:    FIRST page rewritten, OLD tokens before, NEW tokens after
+//   fork:    LENS tokens of the source, or -1 where the call failed
+//   reserve and keep use the other arrays while they plan.
 constexpr int kPlanReserve = 1, kPlanKeep = 2, kPlanFork = 3;
-constexpr int kPlanHeader = 4, kPlanArrays = 7;
-enum { PL_ITEMS = 0, PL_FIRST = 1, PL_TAIL = 2, PL_ROWS = 3, PL_OLD = 2, PL_NEW = 3, PL_START = 4,
-       PL_SPAN = 5, PL_SLOT = 6 };
+constexpr int kPlanHeader = 4, kPlanArrays = 4, kRecord = 8;
+enum { PL_FIRST = 0, PL_OLD = 1, PL_NEW = 2, PL_TAIL = 1, PL_ROWS = 2, PL_SLOT = 3, PL_LENS = 0 };
+// reserve: the page, the page its tokens so far lie in, how many those are, how many it
+// holds now, and the batch's row that would be its token 0 (may be negative).
+enum { RR_PAGE = 0, RR_TAIL = 1, RR_HAD = 2, RR_END = 3, RR_ROW = 4 };
+// keep: the fresh page, the sequence's first token in it, the tokens it holds, the index in
+// the call, the span's start and length, and where its survivors are listed.
+enum { RK_PAGE = 0, RK_POS = 1, RK_END = 2, RK_SEQ = 3, RK_START = 4, RK_SPAN = 5, RK_OFF = 6, RK_COUNT = 7 };
 
-__host__ __device__ inline size_t plan_ints(int n, int max_pages) {
-    return kPlanHeader + (size_t)kPlanArrays * (n + 1) + 2 * (size_t)n * max_pages;
+// Items there can be: pages of the call's tables, and no more than fresh pages and partly
+// filled ones.
+__host__ __device__ inline size_t plan_items(int n, int max_pages, int num_pages) {
+    const size_t a = (size_t)n * max_pages, b = (size_t)num_pages + n;
+    return a < b ? a : b;
+}
+__host__ __device__ inline size_t plan_ints(int n, int max_pages, int num_pages) {
+    return kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages +
+           kRecord * plan_items(n, max_pages, num_pages);
 }
 __device__ __forceinline__ int* plan_array(int* plan, int n, int a) {
     return plan + kPlanHeader + (size_t)a * (n + 1);
@@ -68,12 +80,11 @@ __device__ __forceinline__ int* plan_pages(int* plan, int n, int max_pages, int 
 __device__ __forceinline__ const int* plan_pages(const int* plan, int n, int max_pages, int i) {
     return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)i * max_pages;
 }
-// The sequence of every page item (at most n * max_pages of them).
-__device__ __forceinline__ int* plan_owner(int* plan, int n, int max_pages) {
-    return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages;
+__device__ __forceinline__ int* plan_record(int* plan, int n, int max_pages, int item) {
+    return plan_pages(plan, n, max_pages, n) + (size_t)item * kRecord;
 }
-__device__ __forceinline__ const int* plan_owner(const int* plan, int n, int max_pages) {
-    return plan + kPlanHeader + (size_t)kPlanArrays * (n + 1) + (size_t)n * max_pages;
+__device__ __forceinline__ const int* plan_record(const int* plan, int n, int max_pages, int item) {
+    return plan_pages(plan, n, max_pages, n) + (size_t)item * kRecord;
 }
 // The last i in [0, n) with prefix[i] <= x: the sequence that item x belongs to.
 __device__ __forceinline__ int owner_of(const int* prefix, int n, int x) {
@@ -137,12 +148,14 @@ struct AttendArgs {
     int H, g;                    // query heads, query heads per key head
     int causal;
     float scale2;                // softmax scale * log2(e)
-    int chunk, splits;           // keys per split (a multiple of 32) and splits the launch has
+    int ranges;                  // few rows: ranges of work per key head; many: parts of a block
+    int slots, num_cuts;         // slots for parts per key head; places in the list of cut blocks
     const unsigned short* q;
     unsigned short* out;
     long long q_stride, out_stride;     // elements
     float* lse;
-    float *part_o, *part_l;      // [row][H][split][d], [row][H][split], or null with one split
+    float *part_o, *part_l;      // [Hkv][slots][block rows][dp], [Hkv][slots][block rows]
+    int4* cuts;                  // [num_cuts]
 };
 
 hipError_t launch_rotate(const RotArgs& a, int f32, int vec, hipStream_t s);
@@ -163,7 +176,11 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,
                              const int* idx, const int* off, hipStream_t s);
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
-void attend_splits(const CacheView& c, const BatchView& b, int H, long long max_tokens, int* chunk,
-                   int* splits);
+// Rows of a row block, division of the work and what it keeps of parts, for the form that a
+// call takes.
+int attend_block_rows(const CacheView& c, const BatchView& b, int H);
+int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens);
+void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
+                  long long* cuts);
 
 }  // namespace occam

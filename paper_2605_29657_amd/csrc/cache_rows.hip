@@ -121,8 +121,6 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
     const int n = b.n, G = 1 << p.shift;
     if (plan[0] != kPlanReserve || plan[1] != n) return;
     const int items = plan[2];
-    const int* pre = plan_array(plan, n, PL_ITEMS);
-    const int* owner = plan_owner(plan, n, p.max_pages);
     const int units = (G >> 2) * (c.dp >> 3), span = units < kRowThreads ? units : kRowThreads;
     const int side = kRowThreads / span;                 // blocks of this workgroup at a time
     const int shift = c.dp == 64 ? 3 : c.dp == 128 ? 4 : 5;            // units per group of tokens
@@ -130,22 +128,16 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
     constexpr int ESZ = F32 ? 4 : 2;
     for (int w0 = blockIdx.x * side; w0 < total; w0 += gridDim.x * side) {
         const Block bl = block_at(w0 + threadIdx.x / span, items, c.Hkv);
-        const int i = owner[bl.item];
-        const int len = plan_array(plan, n, PL_FIRST)[i], rows = plan_array(plan, n, PL_ROWS)[i];
-        const int j = (len >> p.shift) + bl.item - pre[i];
-        const int page = p.table[(size_t)plan_array(plan, n, PL_SLOT)[i] * p.max_pages + j];
-        const int pos0 = j << p.shift;
-        const int had = len > pos0 ? len - pos0 : 0;     // tokens the page held
-        const int tail = had ? plan_array(plan, n, PL_TAIL)[i] : page;
+        const int* rec = plan_record(plan, n, p.max_pages, bl.item);
+        const int page = rec[RR_PAGE], tail = rec[RR_TAIL], row0 = rec[RR_ROW];
+        const int had = rec[RR_HAD], end = rec[RR_END];  // tokens the page held, and holds now
         const size_t at = (size_t)page * c.Hkv + bl.head, from = (size_t)tail * c.Hkv + bl.head;
         unsigned char* blk = (bl.kv ? c.v : c.k) + at * c.block;
         const unsigned char* src = (bl.kv ? c.v : c.k) + from * c.block;
         float* scale = bl.kv ? c.vs : c.ks;
         const long long st = bl.kv ? vst : kst;
         // Row of the page's token 0 in the packed rows, at this head.
-        const char* x = (bl.kv ? v : k) +
-                        (((long long)row_begin(b, i) - len + pos0) * st + (long long)bl.head * c.d) * ESZ;
-        const int end = len + rows - pos0 < G ? len + rows - pos0 : G;     // tokens it holds now
+        const char* x = (bl.kv ? v : k) + (row0 * st + (long long)bl.head * c.d) * ESZ;
         Row8<F32> raw[KEEP ? UPT : 1][4];
         auto load = [&](int u, Row8<F32>* r) {
             const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
@@ -247,117 +239,135 @@ __global__ __launch_bounds__(kRowThreads) void cache_read(PageView p, CacheView 
     }
 }
 
-// The source token of the compacted sequence's token x.
+// A span's survivors: token r of them is token start + idx[r] of the sequence.
 struct Kept {
     int start, span, count;
     const int* idx;
 };
-__device__ __forceinline__ int source_of(const Kept& s, int x) {
-    const int r = x - s.start;
-    if (r < 0) return x;
-    if (r >= s.count) return x - s.count + s.span;
-    int v = s.idx[r];
-    v = v < 0 ? 0 : v >= s.span ? s.span - 1 : v;        // never outside the old pages
-    return s.start + v;
-}
 
-// Codes and their scales stay in registers between the search and the conversion (12 per
-// unit).
-template <int UPT>
+// What bounds the move is the chain of loads that finds a token (item, sequence, index,
+// page) before its codes can be read.  It is the same for all heads, so a workgroup follows
+// it once for HG heads of an item's keys or values and then has all their codes in flight;
+// they stay in registers between the search for the scale and the conversion (12 per unit).
+// A block takes `span` threads; workgroups with room for several take several head groups.
+template <int UPT, int HG>
 __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView c, int n,
-                                                          const int* plan, const int* idx,
-                                                          const int* off) {
+                                                          const int* plan, const int* idx) {
     __shared__ float red[kRowThreads / 64];
     if (plan[0] != kPlanKeep || plan[1] != n) return;
     const int items = plan[2], G = 1 << p.shift;
-    const int* pre = plan_array(plan, n, PL_ITEMS);
-    const int* owner = plan_owner(plan, n, p.max_pages);
     const int units = (G >> 2) * (c.dp >> 3), span = units < kRowThreads ? units : kRowThreads;
     const int shift = c.dp == 64 ? 3 : c.dp == 128 ? 4 : 5;
-    const int side = kRowThreads / span, total = items * c.Hkv * 2;
+    const int groups = (c.Hkv + HG - 1) / HG;
+    const int side = kRowThreads / span, total = items * groups * 2;
     for (int w0 = blockIdx.x * side; w0 < total; w0 += gridDim.x * side) {
-        const Block bl = block_at(w0 + threadIdx.x / span, items, c.Hkv);
-        const int i = owner[bl.item];
-        const int first = plan_array(plan, n, PL_FIRST)[i], now = plan_array(plan, n, PL_NEW)[i];
-        const int* olds = plan_pages(plan, n, p.max_pages, i);
-        const int j = first + bl.item - pre[i];
-        const Kept kept{plan_array(plan, n, PL_START)[i], plan_array(plan, n, PL_SPAN)[i],
-                        off[i + 1] - off[i], idx + off[i]};
-        const int pos0 = j << p.shift, end = now - pos0 < G ? now - pos0 : G;
-        const int page = p.table[(size_t)plan_array(plan, n, PL_SLOT)[i] * p.max_pages + j];
+        const Block bl = block_at(w0 + threadIdx.x / span, items, groups);
+        const int head0 = bl.head * HG;
+        const int* rec = plan_record(plan, n, p.max_pages, bl.item);
+        const int* olds = plan_pages(plan, n, p.max_pages, rec[RK_SEQ]);
+        const Kept kept{rec[RK_START], rec[RK_SPAN], rec[RK_COUNT], idx + rec[RK_OFF]};
+        const int page = rec[RK_PAGE], pos0 = rec[RK_POS], end = rec[RK_END];
         unsigned char* store = bl.kv ? c.v : c.k;
         float* scale = bl.kv ? c.vs : c.ks;
-        u32x2 code[UPT][4];                     // eight codes of a token
-        float sc[UPT][4], top = 0.f;
-        // Where the tokens come from, then their codes and scales, all at once.
+        u32x2 code[HG][UPT][4];                 // eight codes of a token
+        float sc[HG][UPT][4];
 #pragma unroll
         for (int y = 0; y < UPT; ++y) {
             const int u = y * span + threadIdx.x % span;
             const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
-            int from[4];
-            size_t at[4];
+            // No branches: a place without a token reads what the page's first one reads, and
+            // drops it, so that all loads of a thread are in flight together.
+            int in[4], old[4];
+            bool is[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int tok = quad * 4 + t;
-                from[t] = bl.live && tok < end ? source_of(kept, pos0 + tok) : -1;
+                is[t] = bl.live && tok < end;
+                // The source of the compacted sequence's token: itself before the span, behind
+                // it moved by what was dropped, listed within (any valid address elsewhere).
+                const int to = pos0 + (is[t] ? tok : 0), r = to - kept.start;
+                int v = *(r >= 0 && r < kept.count ? kept.idx + r : rec);
+                v = v < 0 ? 0 : v >= kept.span ? kept.span - 1 : v;    // never outside the old pages
+                in[t] = r < 0 ? to : r >= kept.count ? to - kept.count + kept.span : kept.start + v;
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                at[t] = from[t] < 0 ? 0 : (size_t)olds[from[t] >> p.shift] * c.Hkv + bl.head;
+            for (int t = 0; t < 4; ++t) old[t] = olds[in[t] >> p.shift];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                code[y][t] = u32x2{0, 0};
-                sc[y][t] = 1.f;
-                if (from[t] < 0) continue;
-                sc[y][t] = scale[at[t]];
-                const int in = from[t] & (G - 1);
-                const unsigned char* blk = store + at[t] * c.block;
+            for (int t = 0; t < 4; ++t) in[t] &= G - 1;
+#pragma unroll
+            for (int x = 0; x < HG; ++x) {
+                const int head = head0 + x < c.Hkv ? head0 + x : c.Hkv - 1;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sc[x][y][t] = scale[(size_t)old[t] * c.Hkv + head];
                 if (bl.kv) {
-                    const unsigned char* w = blk + ((size_t)(in >> 2) * c.dp + e0) * 4;
-                    const u32x4 a = reinterpret_cast<const u32x4*>(w)[0];
-                    const u32x4 b = reinterpret_cast<const u32x4*>(w)[1];
-                    const int sh = (in & 3) * 8;
+                    u32x4 a[4], b[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        code[y][t][0] |= (a[e] >> sh & 255u) << (8 * e);
-                        code[y][t][1] |= (b[e] >> sh & 255u) << (8 * e);
+                    for (int t = 0; t < 4; ++t) {
+                        const unsigned char* w = store + ((size_t)old[t] * c.Hkv + head) * c.block +
+                                                 ((size_t)(in[t] >> 2) * c.dp + e0) * 4;
+                        a[t] = reinterpret_cast<const u32x4*>(w)[0];
+                        b[t] = reinterpret_cast<const u32x4*>(w)[1];
+                    }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        // Byte in & 3 of every dword.
+                        const unsigned pick = 0x0c0c0000u | (4u + (in[t] & 3)) << 8 | (unsigned)(in[t] & 3);
+                        const unsigned a01 = __builtin_amdgcn_perm(a[t][1], a[t][0], pick);
+                        const unsigned a23 = __builtin_amdgcn_perm(a[t][3], a[t][2], pick);
+                        const unsigned b01 = __builtin_amdgcn_perm(b[t][1], b[t][0], pick);
+                        const unsigned b23 = __builtin_amdgcn_perm(b[t][3], b[t][2], pick);
+                        code[x][y][t] = u32x2{a01 | a23 << 16, b01 | b23 << 16};
                     }
                 } else {
-                    code[y][t] = *reinterpret_cast<const u32x2*>(blk + (size_t)in * c.dp + e0);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        code[x][y][t] = *reinterpret_cast<const u32x2*>(
+                            store + ((size_t)old[t] * c.Hkv + head) * c.block + (size_t)in[t] * c.dp + e0);
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    code[x][y][t][0] = is[t] ? code[x][y][t][0] : 0;
+                    code[x][y][t][1] = is[t] ? code[x][y][t][1] : 0;
+                    sc[x][y][t] = is[t] ? sc[x][y][t] : 1.f;
                 }
             }
         }
 #pragma unroll
-        for (int y = 0; y < UPT; ++y)
+        for (int x = 0; x < HG; ++x) {
+            float top = 0.f;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const f32x4 q = dec4(code[y][t][0]), r = dec4(code[y][t][1]);
-                float m = 0.f;
+            for (int y = 0; y < UPT; ++y)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(q[e]), fabsf(r[e])));
-                top = fmaxf(top, m * sc[y][t]);
+                for (int t = 0; t < 4; ++t) {
+                    const f32x4 q = dec4(code[x][y][t][0]), r = dec4(code[x][y][t][1]);
+                    float m = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(q[e]), fabsf(r[e])));
+                    top = fmaxf(top, m * sc[x][y][t]);
+                }
+            top = group_max(top, span, red);
+            const int newexp = scale_exp(top);
+            if (!bl.live || head0 + x >= c.Hkv) continue;
+            const size_t at = (size_t)page * c.Hkv + head0 + x;
+#pragma unroll
+            for (int y = 0; y < UPT; ++y) {
+                const int u = y * span + threadIdx.x % span;
+                const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
+                if (quad * 4 >= end) continue;
+                float z[32];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    int d = exp_of(sc[x][y][t]) - newexp;
+                    d = d < -126 ? -126 : d > 127 ? 127 : d;       // 127: a block of zeros
+                    const float f = exp_scale(d);
+                    const f32x4 q = dec4(code[x][y][t][0]), r = dec4(code[x][y][t][1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { z[t * 8 + e] = q[e] * f; z[t * 8 + 4 + e] = r[e] * f; }
+                }
+                store_codes(store + at * c.block, bl.kv, c.dp, quad, e0, z);
             }
-        top = group_max(top, span, red);
-        const int newexp = scale_exp(top);
-        if (!bl.live) continue;
-#pragma unroll
-        for (int y = 0; y < UPT; ++y) {
-            const int u = y * span + threadIdx.x % span;
-            const int quad = u >> shift, e0 = (u - (quad << shift)) * 8;
-            if (quad * 4 >= end) continue;
-            float z[32];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                int d = exp_of(sc[y][t]) - newexp;
-                d = d < -126 ? -126 : d > 127 ? 127 : d;       // 127: a block of zeros
-                const float f = exp_scale(d);
-                const f32x4 q = dec4(code[y][t][0]), r = dec4(code[y][t][1]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { z[t * 8 + e] = q[e] * f; z[t * 8 + 4 + e] = r[e] * f; }
-            }
-            store_codes(store + ((size_t)page * c.Hkv + bl.head) * c.block, bl.kv, c.dp, quad, e0, z);
+            if (threadIdx.x % span == 0) scale[at] = exp_scale(newexp);
         }
-        if (threadIdx.x % span == 0) scale[(size_t)page * c.Hkv + bl.head] = exp_scale(newexp);
     }
 }
 
@@ -412,9 +422,10 @@ hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const
                              const int* idx, const int* off, hipStream_t s) {
     long long pages = (long long)n * p.max_pages;
     if (pages > p.num_pages) pages = p.num_pages;
-    const dim3 grid(row_grid(p, c, pages * c.Hkv * 2));
     return with_units(p, c, [&](auto upt) {
-        return launch(cache_move<decltype(upt)::value>, grid, dim3(kRowThreads), 0, s, p, c, n, plan, idx, off);
+        constexpr int U = decltype(upt)::value, HG = U == 1 ? 4 : U == 2 ? 2 : 1;
+        const dim3 grid(row_grid(p, c, pages * ((c.Hkv + HG - 1) / HG) * 2));
+        return launch(cache_move<U, HG>, grid, dim3(kRowThreads), 0, s, p, c, n, plan, idx);
     });
 }
 

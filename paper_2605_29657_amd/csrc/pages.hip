@@ -18,6 +18,9 @@ namespace {
 // waves at every barrier), 1024 beyond.  What a call reads again of its sequences is kept in
 // LDS for up to kNear of them, in the plan beyond.
 constexpr int kNear = 1024;
+// Table entries of a fork call that one workgroup of 1024 threads copies by itself: 6.2 us
+// for 32 x 73 entries against 7.6 us in two launches, 7.7 against 8.0 us for 64 x 46.
+constexpr int kSmallTables = 4096;
 
 // Exclusive prefix of x over the workgroup (NT threads), and the total.
 template <int NT>
@@ -145,14 +148,6 @@ __device__ __forceinline__ void begin_call(const PageView& p, PlanShared* sh) {
 __device__ __forceinline__ void write_header(int* plan, int kind, int n, int items) {
     plan[0] = kind; plan[1] = n; plan[2] = items; plan[3] = 0;
 }
-// The sequence of every page item, so that the kernels that work on items need no search.
-template <int NT>
-__device__ __forceinline__ void write_owners(const PageView& p, int* plan, int n, const int* prefix,
-                                             int items) {
-    int* owner = plan_owner(plan, n, p.max_pages);
-    for (int x = threadIdx.x; x < items; x += NT) owner[x] = owner_of(prefix, n, x);
-}
-
 __global__ __launch_bounds__(256) void pages_reset(PageView p) {
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i < p.num_pages) p.refs[i] = 0;
@@ -166,7 +161,6 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
     __shared__ PlanShared sh;
     const int n = b.n, G = 1 << p.shift;
     const unsigned word0 = first_word<NT>(p);
-    int* items = plan_array(plan, n, PL_ITEMS);
     int* g_first = plan_array(plan, n, PL_FIRST);
     int* g_tail = plan_array(plan, n, PL_TAIL);
     int* g_rows = plan_array(plan, n, PL_ROWS);
@@ -187,10 +181,10 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
             if ((long long)len + r > ((long long)p.max_pages << p.shift)) bad = OCCAM_PAGES_TOO_LONG;
             else if (r > 0 && (len & (G - 1))) src = p.table[(size_t)s * p.max_pages + (len >> p.shift)];
         }
-        first[i] = g_first[i] = len;
-        tail[i] = g_tail[i] = src;
-        rows[i] = g_rows[i] = bad ? 0 : r;
-        slot[i] = g_slot[i] = s;
+        first[i] = len;
+        tail[i] = src;
+        rows[i] = bad ? 0 : r;
+        slot[i] = s;
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
@@ -202,7 +196,7 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
         return more + (tail[i] >= 0 && p.refs[tail[i]] > 1);
     });
     __syncthreads();
-    int* list = need <= kNear ? sh.list : plan_owner(plan, n, p.max_pages);
+    int* list = need <= kNear ? sh.list : plan_record(plan, n, p.max_pages, 0);
     // A shared last page is replaced by the first page its sequence gets: table entry
     // len / G; otherwise the first one goes behind, at ceil(len / G).
     if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
@@ -212,10 +206,6 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
             const int j = pages - wanted + (r - sh.need[i]);
             p.table[(size_t)slot[i] * p.max_pages + j] = page;
         })) {
-        for (int i = threadIdx.x; i <= n; i += NT) {
-            items[i] = 0;
-            if (i < n) g_rows[i] = 0;
-        }
         if (threadIdx.x == 0) {
             atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
             write_header(plan, kPlanReserve, n, 0);
@@ -237,16 +227,28 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
         return r > 0 ? ((len + r + G - 1) >> p.shift) - (len >> p.shift) : 0;
     });
     __syncthreads();
-    for (int i = threadIdx.x; i <= n; i += NT) items[i] = sh.need[i];
-    write_owners<NT>(p, plan, n, sh.need, total);
+    for (int x = threadIdx.x; x < total; x += NT) {
+        const int i = owner_of(sh.need, n, x), len = first[i];
+        const int j = (len >> p.shift) + x - sh.need[i], pos0 = j << p.shift;
+        const int page = p.table[(size_t)slot[i] * p.max_pages + j];
+        const int had = len > pos0 ? len - pos0 : 0, now = len + rows[i] - pos0;
+        int* r = plan_record(plan, n, p.max_pages, x);
+        r[RR_PAGE] = page;
+        r[RR_TAIL] = had ? tail[i] : page;
+        r[RR_HAD] = had;
+        r[RR_END] = now < G ? now : G;
+        r[RR_ROW] = row_begin(b, i) - len + pos0;
+    }
     if (threadIdx.x == 0) write_header(plan, kPlanReserve, n, total);
 }
 
-template <int NT>
+// COPY: the forks' table rows too (where they are short enough for one workgroup: a launch
+// less).
+template <int NT, bool COPY>
 __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* src, const int* dst,
                                                 int* plan) {
     __shared__ PlanShared sh;
-    int* lens = plan_array(plan, n, PL_ITEMS);
+    int* lens = plan_array(plan, n, PL_LENS);
     begin_call<NT>(p, &sh);
     for (int i = threadIdx.x; i < n; i += NT) {
         const int s = src[i], t = dst[i];
@@ -261,12 +263,22 @@ __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* sr
         if (threadIdx.x == 0) atomicOr(p.status, (int)OCCAM_PAGES_BAD_SEQ);
     }
     if (threadIdx.x == 0) write_header(plan, kPlanFork, n, 0);
+    if (!COPY || sh.bad) return;
+    for (int x = threadIdx.x; x < n * p.max_pages; x += NT) {
+        const int i = x / p.max_pages, j = x - i * p.max_pages, len = lens[i];
+        if (j >= (len + (1 << p.shift) - 1) >> p.shift) continue;
+        const int page = p.table[(size_t)src[i] * p.max_pages + j];
+        p.table[(size_t)dst[i] * p.max_pages + j] = page;
+        atomicAdd(&p.refs[page], 1);
+    }
+    for (int i = threadIdx.x; i < n; i += NT)
+        if (lens[i] > 0) p.length[dst[i]] = lens[i];
 }
 
 __global__ __launch_bounds__(256) void fork_copy(PageView p, int n, const int* src, const int* dst,
                                                  const int* plan) {
     const int i = blockIdx.x;
-    const int len = plan_array(plan, n, PL_ITEMS)[i];
+    const int len = plan_array(plan, n, PL_LENS)[i];
     if (len <= 0) return;
     const int* from = p.table + (size_t)src[i] * p.max_pages;
     int* to = p.table + (size_t)dst[i] * p.max_pages;
@@ -324,7 +336,6 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
     __shared__ PlanShared sh;
     const int G = 1 << p.shift;
     const unsigned word0 = first_word<NT>(p);
-    int* items = plan_array(plan, n, PL_ITEMS);
     int* g_first = plan_array(plan, n, PL_FIRST);
     int* g_olds = plan_array(plan, n, PL_OLD);
     int* g_news = plan_array(plan, n, PL_NEW);
@@ -352,9 +363,6 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         first[i] = g_first[i] = f;
         olds[i] = g_olds[i] = len;
         news[i] = g_news[i] = now;
-        plan_array(plan, n, PL_START)[i] = a;
-        plan_array(plan, n, PL_SPAN)[i] = m;
-        plan_array(plan, n, PL_SLOT)[i] = s;
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
@@ -363,14 +371,14 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         return sh.bad || pages < 0 ? 0 : pages;
     });
     __syncthreads();
-    int* list = need <= kNear ? sh.list : plan_owner(plan, n, p.max_pages);
+    int* list = need <= kNear ? sh.list : plan_record(plan, n, p.max_pages, 0);
     if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
             const int i = owner_of(sh.need, n, r);
             plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
         })) {
-        for (int i = threadIdx.x; i <= n; i += NT) {
-            items[i] = 0;
-            if (i < n) { g_news[i] = olds[i]; g_first[i] = (olds[i] + G - 1) >> p.shift; }
+        for (int i = threadIdx.x; i < n; i += NT) {
+            g_news[i] = olds[i];
+            g_first[i] = (olds[i] + G - 1) >> p.shift;
         }
         if (threadIdx.x == 0) {
             atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
@@ -378,14 +386,26 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         }
         return;
     }
-    for (int i = threadIdx.x; i <= n; i += NT) items[i] = sh.need[i];
-    __syncthreads();                       // the list may lie where the owners go
-    write_owners<NT>(p, plan, n, sh.need, need);
+    __syncthreads();                       // the list may lie where the records go
+    for (int x = threadIdx.x; x < need; x += NT) {
+        const int i = owner_of(sh.need, n, x), j = first[i] + x - sh.need[i];
+        const int now = news[i] - (j << p.shift);
+        int* r = plan_record(plan, n, p.max_pages, x);
+        r[RK_PAGE] = plan_pages(plan, n, p.max_pages, i)[j];
+        r[RK_POS] = j << p.shift;
+        r[RK_END] = now < G ? now : G;
+        r[RK_SEQ] = i;
+        r[RK_START] = start[i];
+        r[RK_SPAN] = span[i];
+        r[RK_OFF] = off[i];
+        r[RK_COUNT] = off[i + 1] - off[i];
+    }
     if (threadIdx.x == 0) write_header(plan, kPlanKeep, n, need);
 }
 
-// Second part, a workgroup per sequence: the fresh pages go into the table, the old ones
-// into the plan's list (the move reads from them), and the old ones' references end.
+// Compaction, second part, a workgroup per sequence: the fresh pages go into the table, the
+// old ones into the plan's list (the move reads from them), and the old ones' references
+// end.
 __global__ __launch_bounds__(256) void keep_swap(PageView p, int n, const int* seq, int* plan) {
     const int i = blockIdx.x, G = 1 << p.shift;
     const int f = plan_array(plan, n, PL_FIRST)[i];
@@ -417,8 +437,11 @@ hipError_t launch_pages_reserve(const PageView& p, const BatchView& b, int* plan
 
 hipError_t launch_pages_fork(const PageView& p, int n, const int* src, const int* dst, int* plan,
                              hipStream_t s) {
-    hipError_t e = n <= 256 ? launch(fork_plan<256>, dim3(1), dim3(256), 0, s, p, n, src, dst, plan)
-                            : launch(fork_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, src, dst, plan);
+    if ((long long)n * p.max_pages <= kSmallTables)
+        return launch(fork_plan<1024, true>, dim3(1), dim3(1024), 0, s, p, n, src, dst, plan);
+    hipError_t e = n <= 256
+        ? launch(fork_plan<256, false>, dim3(1), dim3(256), 0, s, p, n, src, dst, plan)
+        : launch(fork_plan<1024, false>, dim3(1), dim3(1024), 0, s, p, n, src, dst, plan);
     if (e != hipSuccess) return e;
     return launch(fork_copy, dim3(n), dim3(256), 0, s, p, n, src, dst, plan);
 }
@@ -430,10 +453,9 @@ hipError_t launch_pages_free(const PageView& p, int n, const int* seq, hipStream
 hipError_t launch_pages_keep(const PageView& p, int n, const int* seq, const int* start,
                              const int* span, const int* idx, const int* off, int* plan,
                              hipStream_t s) {
-    hipError_t e = n <= 256 ? launch(keep_plan<256>, dim3(1), dim3(256), 0, s, p, n, seq, start, span,
-                                     idx, off, plan)
-                            : launch(keep_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, seq, start, span,
-                                     idx, off, plan);
+    hipError_t e = n <= 256
+        ? launch(keep_plan<256>, dim3(1), dim3(256), 0, s, p, n, seq, start, span, idx, off, plan)
+        : launch(keep_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, seq, start, span, idx, off, plan);
     if (e != hipSuccess) return e;
     return launch(keep_swap, dim3(n), dim3(256), 0, s, p, n, seq, plan);
 }

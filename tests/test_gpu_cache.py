@@ -275,6 +275,20 @@ def test_fork_and_copy_on_write(page, d):
     assert c.pages.refs.sum().item() == 0
 
 
+@pytest.mark.parametrize("max_pages", [40, 9000])
+def test_page_calls_on_short_and_long_tables(max_pages):
+    # One workgroup walks short tables, a workgroup per sequence long ones.
+    c = Cache(5, 16, 1, 64, num_pages=80, max_pages=max_pages)
+    c.append([0, 1], [200, 33])
+    c.fork([0, 1, 0], [2, 3, 4])
+    c.check()
+    c.keep([2, 4], [3, 100], [150, 60], [list(range(0, 150, 4)), list(range(20))])
+    c.check()
+    c.append([2, 0], [5, 5])
+    c.free([0, 2])
+    c.check()
+
+
 def test_free_twice_in_one_call():
     c = Cache(3, 16, 1, 64)
     c.append([0, 1], [20, 40])
@@ -488,6 +502,24 @@ def test_attend_repeats_bitwise_and_on_another_stream():
             got = attend(c, [0, 1, 2, 3], rows, 8, q=q)
         torch.cuda.synchronize()
         assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("fill", [0x00, 0x01, 0x7e, 0xff])
+def test_attend_whatever_the_workspace_held(fill):
+    # Few ranges of work in a workspace sized for many: nothing in it is read before it is
+    # written.
+    c = Cache(3, 64, 2, 128, num_pages=100, max_pages=40)
+    c.append([0, 1, 2], [300, 257, 411])
+    for T in (1, 15):
+        b = cache.Batch(3, rows=T)
+        ws = cache.workspace(c.pages, c.layer, b, 8)
+        ws.fill_(fill)
+        q = torch.randn(3 * T, 8, 128, generator=c.gen, device=DEV).bfloat16()
+        out, lse = torch.empty_like(q), torch.empty(3 * T, 8, device=DEV)
+        cache.attend(c.pages, c.layer, b, q, out, ws, lse=lse)
+        for s in range(3):
+            x = slice(s * T, s * T + T)
+            M.check_attention(M.f64(out[x]), M.f64(lse[x]), M.f64(q[x]), c.k[s].x, c.v[s].x, True)
 
 
 def test_storage_past_4_gib():
