@@ -26,6 +26,7 @@ and after ``occam.prune`` has chosen a sequence's survivors::
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -87,7 +88,7 @@ def lib():
         for name, args in dict(
                 occam_rotary_init=[R, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_double),
                                    ctypes.POINTER(ctypes.c_uint8)],
-                occam_rotate=[R, _i32, _vp, _i32, _i32, _i32, ctypes.POINTER(_Heads), _vp],
+                occam_rotate=[R, _i32, _vp, _i32, _i32, _i32, _vp, _vp],
                 occam_pages_reset=[P, _vp],
                 occam_pages_reserve=[P, B, _vp, _sz, _vp],
                 occam_pages_fork=[P, _i32, _vp, _vp, _vp, _sz, _vp],
@@ -109,6 +110,8 @@ def lib():
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current = torch._C._cuda_getDevice
+_heads = struct.Struct("PPi4xqq").pack          # an occam_heads
 
 
 def _enqueue(fn, device, stream, *args):
@@ -118,7 +121,7 @@ def _enqueue(fn, device, stream, *args):
         stream = _raw_stream(index)
     elif isinstance(stream, torch.cuda.Stream):
         stream = stream.cuda_stream
-    if index == torch.cuda.current_device():
+    if index == _current():
         st = fn(*args, stream)
     else:
         with torch.cuda.device(device):
@@ -196,17 +199,19 @@ def rotate(rotary, positions, src, dst=None, inverse=False, stream=None):
     dev, dt, rows, d = x.device, x.dtype, x.shape[0], rotary.head_dim
     if dt not in _DTYPES or dev.type != "cuda" or positions.numel() != rows * rotary.axes:
         _bad("positions must have %d axes for every row, tensors float32 or bfloat16 on a GPU" % rotary.axes)
-    heads = []
+    heads = b""
     for t, o in zip(src, dst):
         if t.dim() != 3 or t.shape[0] != rows or o.shape != t.shape:
             _bad("every tensor must have the same rows")
         n = t.shape[1]
-        (ps, ss), (pd, sd) = _rows(t, dev, "src", n, d, dt), _rows(o, dev, "dst", n, d, dt)
-        heads.append((ps, pd, n, ss, sd))
+        ps, ss = pd, sd = _rows(t, dev, "src", n, d, dt)
+        if o is not t:
+            pd, sd = _rows(o, dev, "dst", n, d, dt)
+        heads += _heads(ps, pd, n, ss, sd)
     if rows == 0:
         return
     _enqueue(lib().occam_rotate, dev, stream, rotary.ref, rows, _ints(positions, dev, "positions"),
-             1 if inverse else 0, _DTYPES[dt], len(heads), (_Heads * len(heads))(*heads))
+             1 if inverse else 0, _DTYPES[dt], len(src), heads)
 
 
 # ------------------------------------------------------------------------------- pages
