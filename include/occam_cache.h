@@ -152,7 +152,9 @@ occam_status occam_pages_reset(const occam_pages *pages, hipStream_t stream);
 /* Room for the batch's rows behind what its sequences hold: takes pages, raises the
  * lengths, and writes the plan that every layer's occam_cache_append of the step reads.  A
  * partly filled last page that other sequences share is replaced by a page of its own,
- * which the append fills with its tokens.  All rows of the batch or none. */
+ * which the append fills with its tokens.  All rows of the batch or none.  Every layer's
+ * append has to be enqueued before any later call that takes pages (the shared page may
+ * have become free). */
 occam_status occam_pages_reserve(const occam_pages *pages, const occam_batch *batch,
                                  void *plan, size_t plan_bytes, hipStream_t stream);
 
@@ -168,7 +170,8 @@ occam_status occam_pages_free(const occam_pages *pages, int32_t n, const int32_t
 
 /* Drops tokens: of the span_len[i] tokens of seq[i] from token span_start[i] on, those
  * stay whose index within the span is listed in kept_idx[kept_offsets[i] ..
- * kept_offsets[i + 1]), ascending -- the lists of occam_select / occam_prune.  Tokens
+ * kept_offsets[i + 1]), ascending -- the lists of occam_select / occam_prune (what a list
+ * that is not ascending leaves is undefined, but comes from the same sequence).  Tokens
  * outside the span stay.  The pages from the first dropped token's on are replaced by fresh
  * ones, so pages shared with other sequences are not touched; the fresh pages must be free
  * while the old ones are still held.  Every layer's occam_cache_move has to be enqueued
@@ -221,7 +224,7 @@ size_t occam_cache_workspace_size(const occam_pages *pages, const occam_cache *c
  * out: bfloat16 [rows][H][d], rows q_row_stride / out_row_stride elements apart (multiples
  * of 8, 16-byte aligned).  row_lse (nullable): float32 [rows][H], the natural-log softmax
  * normaliser over those keys, in the layout of occam_score's row_lse.  A row that sees no
- * key gets zeros and -infinity.  max_tokens only sizes the launch and the workspace; a
+ * key gets zeros and -infinity.  q and out must not overlap.  max_tokens only sizes the launch and the workspace; a
  * longer sequence is still attended to in full. */
 occam_status occam_cache_attend(const occam_pages *pages, const occam_cache *cache,
                                 const occam_batch *batch, const occam_attention *attention,

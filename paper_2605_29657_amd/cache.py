@@ -323,9 +323,11 @@ def free(pages, seq, stream=None):
 
 def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=None):
     n, dev = seq.numel(), pages.device
+    if kept_offsets.numel() != n + 1:             # move() takes n from it
+        _bad("kept_offsets must have %d elements" % (n + 1))
     _enqueue(lib().occam_pages_keep, dev, stream, pages.ref, n, _ints(seq, dev, "seq"),
              _ints(span_start, dev, "span_start", n), _ints(span_len, dev, "span_len", n),
-             _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets", n + 1),
+             _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets"),
              *_plan(pages, plan))
 
 
@@ -384,7 +386,7 @@ def workspace(pages, layer, batch, num_heads, max_tokens=0):
 def attend(pages, layer, batch, q, out, ws, lse=None, causal=True, softmax_scale=0.0, max_tokens=0,
            stream=None):
     """occam_cache_attend: ``q`` and ``out`` bfloat16 [rows, num_heads, head_dim], ``lse``
-    float32 [rows, num_heads] or None."""
+    float32 [rows, num_heads] or None.  ``q`` and ``out`` must not overlap."""
     dev, H = pages.device, q.shape[1]
     batch.check(dev, q, out, lse)
     qp = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)

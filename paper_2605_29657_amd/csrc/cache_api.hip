@@ -206,7 +206,8 @@ occam_status occam_rotate(const occam_rotary* rotary, int32_t rows, const int32_
         a.t[i] = RotTensor{static_cast<const char*>(t.src), static_cast<char*>(t.dst), t.heads,
                            (int)(heads - t.heads), t.src_row_stride * e, t.dst_row_stride * e};
     }
-    if (heads > 4096) return OCCAM_ERR_UNSUPPORTED;
+    // A launch has fewer than 2^32 threads: 256 for every 2048 (row, pair) angles.
+    if (heads > 4096 || rows / (2048 / r.pairs) >= (1 << 24) - 1) return OCCAM_ERR_UNSUPPORTED;
     if (rows == 0) return OCCAM_OK;
     a.n = n;
     a.heads = (int)heads;
@@ -340,8 +341,8 @@ occam_status occam_cache_move(const occam_pages* pages, const occam_cache* cache
         (st = check_plan(p, n, plan, plan_bytes)) != OCCAM_OK)
         return st;
     if (!given(kept_idx, 4) || !given(kept_offsets, 4)) return OCCAM_ERR_INVALID_ARG;
-    return hip_ok(launch_cache_move(p, c, n, static_cast<const int*>(plan), kept_idx, kept_offsets,
-                                    stream));
+    // (Where the lists begin stands in the plan's records.)
+    return hip_ok(launch_cache_move(p, c, n, static_cast<const int*>(plan), kept_idx, stream));
 }
 
 size_t occam_cache_workspace_size(const occam_pages* pages, const occam_cache* cache,
@@ -376,7 +377,8 @@ occam_status occam_cache_attend(const occam_pages* pages, const occam_cache* cac
         q_row_stride % 8 || out_row_stride % 8 || (row_lse && !aligned(row_lse, 4)))
         return OCCAM_ERR_INVALID_ARG;
     if (ws_bytes < ap.total) return OCCAM_ERR_WORKSPACE;
-    if (!given(workspace, kAlign)) return OCCAM_ERR_INVALID_ARG;
+    // In place would not do: a row's queries are read by several workgroups.
+    if (!given(workspace, kAlign) || q == out) return OCCAM_ERR_INVALID_ARG;
     AttendArgs& a = ap.a;
     a.q = static_cast<const unsigned short*>(q);
     a.out = static_cast<unsigned short*>(out);

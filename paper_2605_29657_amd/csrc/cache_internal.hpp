@@ -174,7 +174,7 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
                              const int* start, int f32, void* k, long long ks, void* v,
                              long long vs, hipStream_t s);
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,
-                             const int* idx, const int* off, hipStream_t s);
+                             const int* idx, hipStream_t s);
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
 // Rows of a row block, division of the work and what it keeps of parts, for the form that a
 // call takes.

@@ -287,7 +287,10 @@ __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView 
                 // it moved by what was dropped, listed within (any valid address elsewhere).
                 const int to = pos0 + (is[t] ? tok : 0), r = to - kept.start;
                 int v = *(r >= 0 && r < kept.count ? kept.idx + r : rec);
-                v = v < 0 ? 0 : v >= kept.span ? kept.span - 1 : v;    // never outside the old pages
+                // An ascending list has idx[r] >= r.  Holding any list to that and to the span
+                // keeps the source within the pages that the plan lists.
+                v = v < r ? r : v;
+                v = v >= kept.span ? kept.span - 1 : v;
                 in[t] = r < 0 ? to : r >= kept.count ? to - kept.count + kept.span : kept.start + v;
             }
 #pragma unroll
@@ -419,7 +422,7 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
 }
 
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,
-                             const int* idx, const int* off, hipStream_t s) {
+                             const int* idx, hipStream_t s) {
     long long pages = (long long)n * p.max_pages;
     if (pages > p.num_pages) pages = p.num_pages;
     return with_units(p, c, [&](auto upt) {

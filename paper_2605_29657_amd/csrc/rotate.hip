@@ -105,8 +105,8 @@ template <typename T, int N, bool ADJ>
 hipError_t go(const RotArgs& a, hipStream_t s) {
     // Rows per workgroup: what the angle table holds, fewer while that leaves the chip empty.
     int per = kRotPairs / a.pairs;
-    while (per > 1 && (a.rows + per - 1) / per < 2048) per >>= 1;
-    return launch(rotate<T, N, ADJ>, dim3((a.rows + per - 1) / per), dim3(kRotThreads), 0, s, a, per);
+    while (per > 1 && (a.rows - 1) / per + 1 < 2048) per >>= 1;
+    return launch(rotate<T, N, ADJ>, dim3((a.rows - 1) / per + 1), dim3(kRotThreads), 0, s, a, per);
 }
 
 template <typename T, int N>

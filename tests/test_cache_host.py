@@ -3,6 +3,7 @@ host makes before anything is enqueued (no call here reaches a launch)."""
 import ctypes
 import os
 import re
+import types
 from fractions import Fraction
 
 import numpy as np
@@ -190,6 +191,12 @@ def test_attention_workspace(L):
     assert L.occam_cache_attend(p, c, huge, a, FAKE, 1024, FAKE, 1024, None, FAKE, 1 << 50, None) == UNSUPPORTED
 
 
+def test_attention_does_not_work_in_place(L):
+    p, c, b, a = pages(), layer(), batch(), attention()
+    size = L.occam_cache_workspace_size(p, c, b, a)
+    assert L.occam_cache_attend(p, c, b, a, FAKE, 1024, FAKE, 1024, None, FAKE, size, None) == INVALID
+
+
 # ------------------------------------------------------------------------------- rotary
 def rotary(d=128, freq=(1.0, 0.5), axis=None, axes=1, adjacent=False):
     return cache.Rotary(d, freq, axis, axes, adjacent)
@@ -253,7 +260,21 @@ def test_bad_rotate_arguments(L):
     assert L.occam_rotate(r.ref, 0, FAKE, 0, 1, 1, h, None) == occam.OK      # nothing to do
 
 
+def test_more_rows_than_a_launch_has_threads(L):
+    r = cache.Rotary(128, [1.0] * 64)
+    h = (cache._Heads * 1)(cache._Heads(FAKE, FAKE, 1, 128, 128))
+    assert L.occam_rotate(r.ref, (1 << 31) - 1, FAKE, 0, 1, 1, h, None) == UNSUPPORTED
+
+
 # ------------------------------------------------------------------- the binding's checks
+def test_binding_wants_one_offset_more_than_sequences():
+    # move() takes the number of sequences from the offsets.
+    two, four = torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    here = types.SimpleNamespace(device=two.device)
+    with pytest.raises(occam.OccamError, match="kept_offsets"):
+        cache.keep(here, two, two, two, four, four, four)
+
+
 def test_binding_refuses_what_is_not_on_the_device():
     with pytest.raises(occam.OccamError):
         cache.Pages(4, 16, 2, 2, device="cpu")

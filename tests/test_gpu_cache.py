@@ -386,6 +386,39 @@ def test_indices_outside_the_span_stay_inside_the_sequence():
     assert c.pages.length.tolist() == [34, 0] and c.pages.status.item() == 0
 
 
+def test_lists_that_do_not_ascend_stay_inside_the_sequence():
+    # The first gap is at 36, in the span's third page; what the list says behind it is held
+    # to the pages from there on.
+    c = Cache(2, 16, 1, 64)
+    c.append([0], [90])
+    listed = list(range(36)) + [50, 7, 7, 0, 49, -3, 48]
+    idx, offs = i32(listed), i32([0, len(listed)])
+    cache.keep(c.pages, i32([0]), i32([10]), i32([60]), idx, offs, c.plan)
+    cache.move(c.pages, c.layer, c.plan, idx, offs)
+    for x in (c.k[0], c.v[0]):
+        x.keep(10, 60, [max(v, r) for r, v in enumerate(listed)])
+    c.check()
+
+
+@pytest.mark.parametrize("n,max_pages", [(300, 16), (1100, 8)])
+def test_calls_of_more_sequences_than_a_wide_workgroup_or_its_memory(n, max_pages):
+    # 300: more than 256, with everything kept at hand; 1100: more sequences and more fresh
+    # pages than a workgroup keeps at hand, in every call.
+    c = Cache(2 * n, 16, 1, 8, num_pages=8 * n, max_pages=max_pages, seed=n)
+    rng = np.random.default_rng(n)
+    order = rng.permutation(n).tolist()
+    c.append(order, rng.integers(0, 50, n).tolist())
+    c.append(order, rng.integers(0, 30, n).tolist())
+    c.fork(order, [n + x for x in range(n)])
+    c.check()
+    spans = [len(c.k[s].x) for s in order]
+    c.keep(order, [0] * n, spans, [sorted(rng.choice(m, m * 3 // 4, replace=False).tolist()) for m in spans])
+    c.check()
+    c.append(order, [1] * n)
+    c.free(order[::2])
+    c.check()
+
+
 def test_many_sequences_and_a_large_pool():
     # More sequences than a workgroup has threads, pages over many words of the map.
     n, page = 2500, 16
@@ -520,6 +553,50 @@ def test_attend_whatever_the_workspace_held(fill):
         for s in range(3):
             x = slice(s * T, s * T + T)
             M.check_attention(M.f64(out[x]), M.f64(lse[x]), M.f64(q[x]), c.k[s].x, c.v[s].x, True)
+
+
+@pytest.mark.parametrize("H", [2, 8])
+def test_attend_more_row_blocks_than_threads(H):
+    n = 300
+    c = Cache(n, 16, 2, 64, num_pages=4096, max_pages=16, seed=H)
+    rng = np.random.default_rng(H)
+    lens = rng.integers(0, 200, n)
+    lens[::7] = 0
+    c.append(list(range(n)), lens.tolist())
+    order = rng.permutation(n).tolist()
+    attend(c, order, [1] * n, H)
+    attend(c, order, rng.integers(0, 8, n).tolist(), H)
+    attend(c, order, rng.integers(0, 9, n).tolist(), H, causal=False)
+    attend(c, order, np.where(np.arange(n) % 50, rng.integers(0, 3, n), 40).tolist(), H)
+
+
+@pytest.mark.parametrize("rows", [[1, 1, 1], [70, 300, 5]])
+def test_attend_captured_and_beside_another_stream(rows):
+    c = Cache(3, 64, 2, 128, num_pages=100, max_pages=40)
+    c.append([0, 1, 2], [400, 900, 33])
+    H, n, b = 8, sum(rows), c.batch([0, 1, 2], rows)
+    q = [torch.randn(n, H, 128, generator=c.gen, device=DEV).bfloat16() for _ in range(2)]
+    ws = [cache.workspace(c.pages, c.layer, b, H) for _ in range(2)]
+    out = [torch.empty_like(x) for x in q]
+    lse = [torch.empty(n, H, device=DEV) for _ in range(2)]
+
+    def call(x):
+        cache.attend(c.pages, c.layer, b, q[x], out[x], ws[x], lse=lse[x])
+
+    want = [attend(c, [0, 1, 2], rows, H, q=x) for x in q]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        call(0)
+    for _ in range(3):
+        for o, z in zip(out, lse):
+            o.zero_(), z.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        with torch.cuda.stream(side):
+            call(1)
+        torch.cuda.synchronize()
+        for x in range(2):
+            assert torch.equal(out[x], want[x][0]) and torch.equal(lse[x], want[x][1])
 
 
 def test_storage_past_4_gib():
