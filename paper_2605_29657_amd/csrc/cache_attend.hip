@@ -783,25 +783,43 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const float f = exp_scale(ref);
     const long long orow = (long long)row_begin(a.b, i) + t;
     const size_t at = ((size_t)h * a.slots + task) * ROWS + wave * 32 + n;
-    unsigned short* out = a.out + orow * a.out_stride + (long long)hh * a.c.d;
+    if (whole) {
+        // Through LDS, a part of the buffers for each wave (no wave reads a tile any more): a
+        // lane's four elements of a row would leave as pieces of 16 bytes.
+        constexpr int PITCH = DP * 2 + 16, RPI = 64 / CH;          // rows per instruction
+        static_assert(WAVES * 32 * PITCH <= many_lds<DP>(), "output tile");
+        unsigned char* o = lds + wave * 32 * PITCH;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-            const int e0 = d * 32 + 8 * e4 + 4 * half;
-            if (!live || e0 >= a.c.d) continue;
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = acc[d][e4 * 4 + e] * inv * f;
-            if (whole) {
-                union { bf16x2 p[2]; u32x2 v; } o;
-                o.p[0] = bf16x2{(__bf16)y[0], (__bf16)y[1]};
-                o.p[1] = bf16x2{(__bf16)y[2], (__bf16)y[3]};
-                *reinterpret_cast<u32x2*>(out + e0) = o.v;
-            } else {
-                *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = f32x4{y[0], y[1], y[2], y[3]};
+            for (int e4 = 0; e4 < 4; ++e4) {
+                union { bf16x2 p[2]; u32x2 v; } y;
+                y.p[0] = bf16x2{(__bf16)(acc[d][e4 * 4] * inv * f), (__bf16)(acc[d][e4 * 4 + 1] * inv * f)};
+                y.p[1] = bf16x2{(__bf16)(acc[d][e4 * 4 + 2] * inv * f), (__bf16)(acc[d][e4 * 4 + 3] * inv * f)};
+                *reinterpret_cast<u32x2*>(o + n * PITCH + (d * 32 + 8 * e4 + 4 * half) * 2) = y.v;
             }
+        const long long to = live ? orow * a.out_stride + (long long)hh * a.c.d : -1;
+        const int chunk = lane & (CH - 1);
+#pragma unroll
+        for (int x = 0; x < 32 / RPI; ++x) {
+            const int r = x * RPI + lane / CH;
+            const long long dst = __shfl(to, r);
+            const u32x4 y = *reinterpret_cast<const u32x4*>(o + r * PITCH + chunk * 16);
+            if (dst >= 0 && chunk * 8 < a.c.d) *reinterpret_cast<u32x4*>(a.out + dst + chunk * 8) = y;
         }
+    } else {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const int e0 = d * 32 + 8 * e4 + 4 * half;
+                if (!live || e0 >= a.c.d) continue;
+                f32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = acc[d][e4 * 4 + e] * inv * f;
+                *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = y;
+            }
+    }
     if (live && half == 0) {
         if (whole) { if (a.lse) a.lse[orow * a.H + hh] = lse2 * kLn2; }
         else a.part_l[at] = lse2;
