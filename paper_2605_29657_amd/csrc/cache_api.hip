@@ -85,6 +85,7 @@ bool rows_ok(const void* x, long long stride, const CacheView& c, int dtype) {
 struct AttendPlan {
     AttendArgs a;
     size_t off_l, off_cuts, total;
+    int ordered;
 };
 
 occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView& b,
@@ -120,6 +121,8 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
         out->off_cuts = align_up(out->off_l + rows * sizeof(float));
         out->total = align_up(out->off_cuts + (size_t)cuts * sizeof(int4));
     }
+    out->ordered = attend_ordered(c, b, a.H, a.ranges);        // (then nothing is cut)
+    if (out->ordered) out->total = align_up(out->ordered * sizeof(AttendBlock));
     if (out->total < kAlign) out->total = kAlign;
     return OCCAM_OK;
 }
@@ -388,6 +391,7 @@ occam_status occam_cache_attend(const occam_pages* pages, const occam_cache* cac
     a.part_o = static_cast<float*>(workspace);
     a.part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + ap.off_l);
     a.cuts = reinterpret_cast<int4*>(static_cast<char*>(workspace) + ap.off_cuts);
+    a.order = ap.ordered ? static_cast<AttendBlock*>(workspace) : nullptr;
     return hip_ok(launch_cache_attend(a, stream));
 }
 

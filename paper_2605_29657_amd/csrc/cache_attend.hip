@@ -62,9 +62,7 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // A row block's keys may be cut into parts; each leaves its output and normaliser in a slot
 // of the workspace, and attend_join puts a block's parts together.
 // ---------------------------------------------------------------------------------------
-struct Block {                     // one row block of one sequence
-    int i, T, len, slot, r0, end;  // end: keys its rows see (0 or less: none)
-};
+typedef AttendBlock Block;
 // Later row blocks of every sequence come first: under a causal mask they are the long ones.
 __device__ __forceinline__ Block block_of(const AttendArgs& a, int entry, int blocks, int rows) {
     Block t;
@@ -456,6 +454,39 @@ __device__ __forceinline__ void lds_barrier() {
 // itself reads two and waits for them).
 constexpr int kReads = 8;
 
+// The row blocks of a ragged batch, longest first: a workgroup that starts late on a long
+// one would end long after the others.  (In which order blocks of one length come is left
+// open; it decides where they run, not what they give.)
+__global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entries, int blocks, int rows) {
+    __shared__ int bin[kMaxOrder], sums[kMaxOrder / 64];
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    bin[e] = 0;
+    __syncthreads();
+    Block b = {};
+    int to = 0, at = 0;
+    if (e < entries) {
+        b = block_of(a, e, blocks, rows);
+        const int units = units_of(a, b, kTile);
+        to = kMaxOrder - 1 - (units < kMaxOrder ? units : kMaxOrder - 1);
+        at = atomicAdd(&bin[to], 1);
+    }
+    __syncthreads();
+    const int own = bin[e];
+    int s = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(s, o);
+        if (lane >= o) s += y;
+    }
+    if (lane == 63) sums[wave] = s;
+    __syncthreads();
+    int before = s - own;
+    for (int w = 0; w < wave; ++w) before += sums[w];
+    bin[e] = before;
+    __syncthreads();
+    if (e < entries) a.order[bin[to] + at] = b;
+}
+
 template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
 template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
 template <int DP> constexpr int many_lds() { return many_bufs<DP>() * 2 * kTile * DP * 2; }
@@ -482,18 +513,18 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const int blocks = (a.b.max_rows * a.g + ROWS - 1) / ROWS;
     const int task = blockIdx.x / a.c.Hkv, h = blockIdx.x - task * a.c.Hkv;
     const int entry = task / a.ranges, part = task - entry * a.ranges;
-    const Block block = block_of(a, entry, blocks, ROWS);
+    const Block block = a.order ? a.order[entry] : block_of(a, entry, blocks, ROWS);
     const int units = units_of(a, block, kTile);
-    int parts = (units + kManyLeast - 1) / kManyLeast;
-    parts = parts < a.ranges ? parts : a.ranges;
+    int each = (units + a.ranges - 1) / a.ranges;              // tiles of a part
+    each = each < kManyLeast ? kManyLeast : each;
+    const int parts = (units + each - 1) / each;
     if (a.slots > 0 && h == 0 && part == 0 && threadIdx.x == 0)
         a.cuts[entry] = int4{parts > 1 ? entry : -1, parts, entry * a.ranges, 1};
     if (part >= parts) return;
     const bool whole = parts == 1;
     const int i = block.i, T = block.T, len = block.len, r0 = block.r0;
-    const int lo = (int)((long long)units * part / parts) * kTile;
-    const int up = (int)((long long)units * (part + 1) / parts) * kTile;
-    const int hi = up < block.end ? up : block.end;
+    const int lo = part * each * kTile;
+    const int hi = block.end - lo < each * kTile ? block.end : lo + each * kTile;
     auto block_end = [&](int first, int rows) {              // keys that these rows see
         if (first >= T * a.g) return 0;
         if (!a.causal) return len;
@@ -507,18 +538,8 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const bool live = t < T;
     const int last = live ? (a.causal ? len - T + t : len - 1) : -1;
 
+    const long long orow = (long long)row_begin(a.b, i) + t;       // of the packed rows
     bf16x8 q[NK];
-    {
-        const long long qrow = (long long)row_begin(a.b, i) + t;
-#pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            const int e = c * 16 + half * 8;
-            u32x4 x = {0, 0, 0, 0};
-            if (live && e < a.c.d)
-                x = *reinterpret_cast<const u32x4*>(a.q + qrow * a.q_stride + (long long)hh * a.c.d + e);
-            q[c] = __builtin_bit_cast(bf16x8, x);
-        }
-    }
     f32x16 acc[ND] = {};
     float m = -INFINITY, l = 0.f;            // m: the maximum in use, in base 2
     int ref = kMinExp;                       // of the values summed; the same in every wave
@@ -559,8 +580,8 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const int x0 = threadIdx.x % DP, hf = x0 / (DP / 2);
     const unsigned koff = x0 * 16, voff = (hf * DP + (x0 - hf * (DP / 2)) * 2) * 4;
     auto group_of = [&](int u) { return (u * THREADS + wave * 64) / DP; };
-    auto load_tile = [&](int pos, const Win& v, Raw& r) {
-        const int g0 = (pos >> 4) & 63;
+    auto load_tile = [&](int tile, const Win& v, Raw& r) {
+        const int g0 = (tile * (kTile / 16)) & 63;
         r.top = __builtin_amdgcn_readlane(v.top, g0);
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
@@ -700,34 +721,61 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     };
     if (hi > lo) {
         const int tiles = (hi - lo + kTile - 1) / kTile;
-        int base = (lo >> 4) & ~63;
+        int base = lo >> 4;                      // windows count from the part's first group
         win.page = win_page(base);
+        nxt.page = win_page(base + 64);
         win_scales(base, win);
-        nxt = win;
         // Tiles past the last one are fetched (page 0's codes) and stored like the others, so
         // that a matrix phase has no branches; nothing reads them.
         auto window = [&](int tile) {
-            const int in = ((lo + tile * kTile) >> 4) & 63;
-            if (((lo + tile * kTile) >> 4 & ~63) != base) { win = nxt; base += 64; }
-            if (in == 0 || tile == 0) nxt.page = win_page(base + 64);
-            if (in == 32 || (tile == 0 && in > 32)) win_scales(base + 64, nxt);
+            const int in = (tile * (kTile / 16)) & 63;
+            if (in == 0) {
+                win = nxt;
+                base += 64;
+                nxt.page = win_page(base + 64);
+            }
+            if (in == 32) win_scales(base + 64, nxt);
         };
-        auto fetch = [&](int tile, Raw& r) { load_tile(lo + tile * kTile, win, r); };
+        auto fetch = [&](int tile, Raw& r) { load_tile(tile, win, r); };
         int refs[AHEAD + 1];                     // of tiles t .. t + AHEAD
         int to = kMinExp;
-        for (int x = 0; x < AHEAD; ++x) {
-            window(x);
-            fetch(x, raw[0]);
-            mask_tile(lo + x * kTile, raw[0]);
-            to = raw[0].top > to ? raw[0].top : to;
-            store_tile(raw[0], x % BUFS, to);
-            refs[x] = to;
+        Raw start[AHEAD];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) fetch(x, start[x]);
+#pragma unroll
+        for (int x = 0; x < SETS; ++x) fetch(AHEAD + x, raw[x]);
+        // Queries: whole rows from memory, after the tiles (loads return in order), turned
+        // into operands through the buffers that no tile is stored to yet.
+        constexpr int RPI = 64 / CH;                               // rows per instruction
+        static_assert(WAVES * 32 * DP * 2 <= (BUFS - AHEAD) * 2 * HALF, "queries in the free buffers");
+        // Rows behind the last one read the sequence's first row; nothing of theirs is written.
+        const long long from = live ? orow * a.q_stride + (long long)hh * a.c.d
+                                    : (long long)row_begin(a.b, i) * a.q_stride + (long long)h * a.g * a.c.d;
+        const int chunk = lane & (CH - 1);
+        const bool inside = chunk * 8 < a.c.d;
+        u32x4 qx[32 / RPI];
+#pragma unroll
+        for (int x = 0; x < 32 / RPI; ++x) {
+            const long long src = __shfl(from, x * RPI + lane / CH);
+            qx[x] = *reinterpret_cast<const u32x4*>(a.q + src + (inside ? chunk * 8 : 0));
         }
 #pragma unroll
-        for (int x = 0; x < SETS; ++x) {
-            window(AHEAD + x);
-            fetch(AHEAD + x, raw[x]);
+        for (int x = 0; x < AHEAD; ++x) {
+            mask_tile(lo + x * kTile, start[x]);
+            to = start[x].top > to ? start[x].top : to;
+            store_tile(start[x], x % BUFS, to);
+            refs[x] = to;
         }
+        unsigned char* qd = lds + AHEAD * 2 * HALF + wave * 32 * DP * 2;
+#pragma unroll
+        for (int x = 0; x < 32 / RPI; ++x) {
+            const int r = x * RPI + lane / CH;
+            if (!inside) qx[x] = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4*>(qd + r * DP * 2 + (chunk ^ (r & (CH < 16 ? CH - 1 : 15))) * 16) = qx[x];
+        }
+#pragma unroll
+        for (int c = 0; c < NK; ++c)
+            q[c] = *reinterpret_cast<const bf16x8*>(qd + n * DP * 2 + ((c * 2 + half) ^ sw) * 16);
         lds_barrier();
         const bool behind = AHEAD == 2 && wave >= 4;
         if (behind) lds_barrier();
@@ -781,7 +829,6 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) - kManyLift : -INFINITY;
     const float f = exp_scale(ref);
-    const long long orow = (long long)row_begin(a.b, i) + t;
     const size_t at = ((size_t)h * a.slots + task) * ROWS + wave * 32 + n;
     if (whole) {
         // Through LDS, a part of the buffers for each wave (no wave reads a tile any more): a
@@ -917,6 +964,15 @@ int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_t
     return want < 1 ? 1 : (int)want;
 }
 
+// Whether a call sorts its row blocks: one more launch, where rows differ from sequence to
+// sequence and there are blocks for more than a round of the chip, up to a number whose
+// unevenness still shows at the end.
+int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges) {
+    const long long entries = b.n * attend_blocks(c, b, H);
+    return b.off && ranges == 1 && attend_block_rows(c, b, H) > kFewRows && entries > 1 && entries <= kMaxOrder
+               ? (int)entries : 0;
+}
+
 // Slots for parts per key head, and places in the list of cut blocks: none where nothing
 // can be cut.
 void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
@@ -937,6 +993,11 @@ static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
     if (few) {
         e = launch(attend_few<DP>, grid, dim3(64 * kFewWaves), 0, s, a);
     } else {
+        if (a.order) {
+            const int blocks = (int)attend_blocks(a.c, a.b, a.H);
+            e = launch(attend_order, dim3(1), dim3(kMaxOrder), 0, s, a, a.b.n * blocks, blocks, br);
+            if (e != hipSuccess) return e;
+        }
         static_assert(32 * many_waves<DP>() == (DP == 128 ? 256 : 128), "rows of a block");
         constexpr int bytes = many_lds<DP>();
         static std::atomic<uint64_t> done{0};

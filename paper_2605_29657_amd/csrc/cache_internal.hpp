@@ -141,6 +141,13 @@ struct RotArgs {
     unsigned char axis[OCCAM_MAX_PAIRS];
 };
 
+// One row block of one sequence: its place in the batch, rows, length, slot, first row, and
+// the keys that its rows see (0 or less: none).
+struct AttendBlock {
+    int i, T, len, slot, r0, end;
+};
+constexpr int kMaxOrder = 1024;          // row blocks that a call sorts by length at most
+
 struct AttendArgs {
     PageView pg;
     CacheView c;
@@ -156,6 +163,7 @@ struct AttendArgs {
     float* lse;
     float *part_o, *part_l;      // [Hkv][slots][block rows][dp], [Hkv][slots][block rows]
     int4* cuts;                  // [num_cuts]
+    AttendBlock* order;          // row blocks, longest first, or NULL: as block_of numbers them
 };
 
 hipError_t launch_rotate(const RotArgs& a, int f32, int vec, hipStream_t s);
@@ -176,10 +184,11 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,
                              const int* idx, hipStream_t s);
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
-// Rows of a row block, division of the work and what it keeps of parts, for the form that a
-// call takes.
+// Rows of a row block, division of the work, row blocks that are sorted (0: as they come) and
+// what is kept of parts, for the form that a call takes.
 int attend_block_rows(const CacheView& c, const BatchView& b, int H);
 int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens);
+int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges);
 void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
                   long long* cuts);
 
