@@ -110,6 +110,7 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     if ((double)b.n * ((double)b.max_rows * a.g / 16 + 1) * ((double)cap / 64 + 1) >= 2147483648.0)
         return OCCAM_ERR_UNSUPPORTED;
     a.ranges = attend_ranges(c, b, a.H, most);
+    a.stream = attend_streams(c, b, a.H, most);
     long long slots, cuts;
     attend_slots(c, b, a.H, a.ranges, &slots, &cuts);
     if (cuts > 65535) return OCCAM_ERR_UNSUPPORTED;        // a launch's grid.y

@@ -187,7 +187,7 @@ struct Window {
     float ks, vs;
 };
 
-template <int DP>
+template <int DP, bool STREAM>
 __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) void attend_few(AttendArgs a) {
     constexpr int NC = DP / 64;            // 64-element chunks of a row
     __shared__ float jo[kFewWaves][kFewRows][64 + 4];
@@ -263,8 +263,8 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
             const unsigned char* vp = a.c.v + off + g4 * DP * 4 + n * 16;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                x.k[u][c] = *reinterpret_cast<const u32x4*>(kp + c * 64);
-                x.v[u][c] = *reinterpret_cast<const u32x4*>(vp + c * 256);
+                x.k[u][c] = get<STREAM>(reinterpret_cast<const u32x4*>(kp + c * 64));
+                x.v[u][c] = get<STREAM>(reinterpret_cast<const u32x4*>(vp + c * 256));
             }
         }
         // The scales after the codes, which need only the page numbers of a new window.
@@ -964,6 +964,15 @@ int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_t
     return want < 1 ? 1 : (int)want;
 }
 
+// Whether the few-row form reads the codes past the caches: where nothing reads them twice
+// (one row block per sequence and key head) and they may be more than the last-level cache
+// holds.  64 x 4096 tokens of 8 heads take 96 us against 106, with two row blocks each 208
+// against 177 us; 4 x 2048 tokens 14.7 against 14.3 us.
+int attend_streams(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
+    return attend_block_rows(c, b, H) == kFewRows && attend_blocks(c, b, H) == 1 &&
+           2 * b.n * max_tokens * c.Hkv * c.dp > kLastLevelBytes;
+}
+
 // Whether a call sorts its row blocks: one more launch, where rows differ from sequence to
 // sequence and there are blocks for more than a round of the chip, up to a number whose
 // unevenness still shows at the end.
@@ -991,7 +1000,7 @@ static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)(tasks * a.c.Hkv));
     hipError_t e;
     if (few) {
-        e = launch(attend_few<DP>, grid, dim3(64 * kFewWaves), 0, s, a);
+        e = launch(a.stream ? attend_few<DP, true> : attend_few<DP, false>, grid, dim3(64 * kFewWaves), 0, s, a);
     } else {
         if (a.order) {
             const int blocks = (int)attend_blocks(a.c, a.b, a.H);

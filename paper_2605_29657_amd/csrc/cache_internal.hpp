@@ -126,6 +126,20 @@ __device__ __forceinline__ int exp_of(float scale) {       // of a power of two
     return (int)((__float_as_uint(scale) >> 23) & 255) - 127;
 }
 
+// What a call touches once and is larger than the last-level cache goes past the caches: it
+// would push out everything else, itself included.
+constexpr long long kLastLevelBytes = 256ll << 20;
+template <bool STREAM, typename V>
+__device__ __forceinline__ V get(const V* from) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(from);
+    else return *from;
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void put(V x, V* to) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, to);
+    else *to = x;
+}
+
 struct RotTensor {
     const char* src;
     char* dst;
@@ -156,6 +170,7 @@ struct AttendArgs {
     int causal;
     float scale2;                // softmax scale * log2(e)
     int ranges;                  // few rows: ranges of work per key head; many: parts of a block
+    int stream;                  // few rows: the codes are read past the caches
     int slots, num_cuts;         // slots for parts per key head; places in the list of cut blocks
     const unsigned short* q;
     unsigned short* out;
@@ -188,6 +203,7 @@ hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
 // what is kept of parts, for the form that a call takes.
 int attend_block_rows(const CacheView& c, const BatchView& b, int H);
 int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens);
+int attend_streams(const CacheView& c, const BatchView& b, int H, long long max_tokens);
 int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges);
 void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
                   long long* cuts);

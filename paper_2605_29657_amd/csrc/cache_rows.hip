@@ -79,9 +79,15 @@ __device__ __forceinline__ void store_codes(unsigned char* blk, bool val, int dp
 template <bool F32>
 struct Row8 {
     u32x4 w[F32 ? 2 : 1];
+    // ONCE: nothing reads them again here (the caches are left to the codes: 224 us against
+    // 227 us for 40000 tokens with their reading back).
+    template <bool ONCE>
     __device__ __forceinline__ void load(const char* p) {
-        w[0] = reinterpret_cast<const u32x4*>(p)[0];
-        if constexpr (F32) w[1] = reinterpret_cast<const u32x4*>(p)[1];
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) {
+            const u32x4* x = reinterpret_cast<const u32x4*>(p) + i;
+            w[i] = get<ONCE>(x);
+        }
     }
     __device__ __forceinline__ void zero() {
         w[0] = u32x4{0, 0, 0, 0};
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int tok = quad * 4 + t;
-                if (bl.live && e0 < c.d && tok >= had && tok < end) r[t].load(x + (tok * st + e0) * ESZ);
+                if (bl.live && e0 < c.d && tok >= had && tok < end) r[t].template load<KEEP>(x + (tok * st + e0) * ESZ);
                 else r[t].zero();
             }
         };
@@ -191,7 +197,10 @@ __global__ __launch_bounds__(kRowThreads) void cache_append(PageView p, CacheVie
     }
 }
 
-template <bool F32>
+// STREAM: for outputs larger than the last-level cache.  2 x 134 MB take 60 us against 71,
+// 137 against 145 us with an addition of the two behind it; at 2 x 67 MB both ways take
+// 31.5 us, but 63.5 against 61.3 us with the addition.
+template <bool F32, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void cache_read(PageView p, CacheView c, BatchView b,
                                                           const int* start, char* k, long long kst,
                                                           char* v, long long vst) {
@@ -224,8 +233,9 @@ __global__ __launch_bounds__(kRowThreads) void cache_read(PageView p, CacheView 
             char* to = out + (row * st + (long long)head * c.d + e0) * (F32 ? 4 : 2);
             const float* x = y + t * 8;
             if constexpr (F32) {
-                reinterpret_cast<f32x4*>(to)[0] = f32x4{x[0] * sc, x[1] * sc, x[2] * sc, x[3] * sc};
-                reinterpret_cast<f32x4*>(to)[1] = f32x4{x[4] * sc, x[5] * sc, x[6] * sc, x[7] * sc};
+                f32x4* o = reinterpret_cast<f32x4*>(to);
+                put<STREAM>(f32x4{x[0] * sc, x[1] * sc, x[2] * sc, x[3] * sc}, o);
+                put<STREAM>(f32x4{x[4] * sc, x[5] * sc, x[6] * sc, x[7] * sc}, o + 1);
             } else {
                 // Exact: the low 16 bits are zero (4 significant bits, normal numbers only).
                 u32x4 w;
@@ -233,7 +243,7 @@ __global__ __launch_bounds__(kRowThreads) void cache_read(PageView p, CacheView 
                 for (int e = 0; e < 4; ++e)
                     w[e] = (__float_as_uint(x[2 * e] * sc) >> 16) |
                            (__float_as_uint(x[2 * e + 1] * sc) & 0xffff0000u);
-                *reinterpret_cast<u32x4*>(to) = w;
+                put<STREAM>(w, reinterpret_cast<u32x4*>(to));
             }
         }
     }
@@ -417,8 +427,13 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
     const long long units = (most / 4 + 2) * c.Hkv * (c.d / 8);
     const dim3 grid((unsigned)((units + kRowThreads - 1) / kRowThreads), b.n);
     auto kk = static_cast<char*>(k), vv = static_cast<char*>(v);
-    return f32 ? launch(cache_read<true>, grid, dim3(kRowThreads), 0, s, p, c, b, start, kk, ks, vv, vs)
-               : launch(cache_read<false>, grid, dim3(kRowThreads), 0, s, p, c, b, start, kk, ks, vv, vs);
+    const long long bytes = b.n * most * c.Hkv * c.d * (f32 ? 4 : 2) * ((k != nullptr) + (v != nullptr));
+    const bool stream = bytes > kLastLevelBytes;
+    auto go = [&](auto kernel) {
+        return launch(kernel, grid, dim3(kRowThreads), 0, s, p, c, b, start, kk, ks, vv, vs);
+    };
+    if (f32) return stream ? go(cache_read<true, true>) : go(cache_read<true, false>);
+    return stream ? go(cache_read<false, true>) : go(cache_read<false, false>);
 }
 
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,

@@ -32,9 +32,23 @@ template <> __device__ __forceinline__ unsigned short from_f(float x) {
 template <typename T, int N>
 struct alignas(sizeof(T) * N) Pack { T x[N]; };
 
+// STREAM: for tensors larger than the last-level cache, in units of 16 bytes: 2 x 362 MB take
+// 152 us against 159; at 2 x 151 MB, 80 us against 71.
+template <bool STREAM, typename T, int N>
+__device__ __forceinline__ Pack<T, N> load(const T* p) {
+    typedef Pack<T, N> V;
+    if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, get<STREAM>(reinterpret_cast<const u32x4*>(p)));
+    else return *reinterpret_cast<const V*>(p);
+}
+template <bool STREAM, typename T, int N>
+__device__ __forceinline__ void store(const Pack<T, N>& x, T* p) {
+    if constexpr (sizeof(x) == 16) put<STREAM>(__builtin_bit_cast(u32x4, x), reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<Pack<T, N>*>(p) = x;
+}
+
 // N elements per unit (a power of two; both sides of N pairs for HALVES, N / 2 pairs for
 // ADJACENT when N > 1).
-template <typename T, int N, bool ADJ>
+template <typename T, int N, bool ADJ, bool STREAM>
 __global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
     __shared__ float2 cs[kRotPairs];
     const int row0 = blockIdx.x * rows_per;
@@ -66,7 +80,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
         if (w >= np) {
             if (x == y) continue;
             const int e = 2 * a.pairs + (w - np) * N;
-            *reinterpret_cast<V*>(y + e) = *reinterpret_cast<const V*>(x + e);
+            store<STREAM>(load<STREAM, T, N>(x + e), y + e);
             continue;
         }
         const float2* f = cs + r * a.pairs;
@@ -76,7 +90,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
             y[2 * w] = from_f<T>(p0 * q.x - p1 * q.y);
             y[2 * w + 1] = from_f<T>(p0 * q.y + p1 * q.x);
         } else if constexpr (ADJ) {
-            V v = *reinterpret_cast<const V*>(x + w * N);
+            V v = load<STREAM, T, N>(x + w * N);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 const float2 q = f[w * (N / 2) + i];
@@ -84,10 +98,10 @@ __global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
                 v.x[2 * i] = from_f<T>(p0 * q.x - p1 * q.y);
                 v.x[2 * i + 1] = from_f<T>(p0 * q.y + p1 * q.x);
             }
-            *reinterpret_cast<V*>(y + w * N) = v;
+            store<STREAM>(v, y + w * N);
         } else {
-            V v0 = *reinterpret_cast<const V*>(x + w * N);
-            V v1 = *reinterpret_cast<const V*>(x + a.pairs + w * N);
+            V v0 = load<STREAM, T, N>(x + w * N);
+            V v1 = load<STREAM, T, N>(x + a.pairs + w * N);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float2 q = f[w * N + i];
@@ -95,8 +109,8 @@ __global__ __launch_bounds__(kRotThreads) void rotate(RotArgs a, int rows_per) {
                 v0.x[i] = from_f<T>(p0 * q.x - p1 * q.y);
                 v1.x[i] = from_f<T>(p0 * q.y + p1 * q.x);
             }
-            *reinterpret_cast<V*>(y + w * N) = v0;
-            *reinterpret_cast<V*>(y + a.pairs + w * N) = v1;
+            store<STREAM>(v0, y + w * N);
+            store<STREAM>(v1, y + a.pairs + w * N);
         }
     }
 }
@@ -106,7 +120,11 @@ hipError_t go(const RotArgs& a, hipStream_t s) {
     // Rows per workgroup: what the angle table holds, fewer while that leaves the chip empty.
     int per = kRotPairs / a.pairs;
     while (per > 1 && (a.rows - 1) / per + 1 < 2048) per >>= 1;
-    return launch(rotate<T, N, ADJ>, dim3((a.rows - 1) / per + 1), dim3(kRotThreads), 0, s, a, per);
+    const dim3 grid((a.rows - 1) / per + 1);
+    if constexpr (sizeof(T) * N == 16)
+        if ((long long)a.rows * a.heads * a.d * (long long)sizeof(T) > kLastLevelBytes)
+            return launch(rotate<T, N, ADJ, true>, grid, dim3(kRotThreads), 0, s, a, per);
+    return launch(rotate<T, N, ADJ, false>, grid, dim3(kRotThreads), 0, s, a, per);
 }
 
 template <typename T, int N>
