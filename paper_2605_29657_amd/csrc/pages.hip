@@ -16,29 +16,29 @@ namespace {
 
 // Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences (fewer
 // waves at every barrier), 1024 beyond.  What a call reads again of its sequences is kept in
-// LDS for up to kNear of them, in the plan beyond.
-constexpr int kNear = 1024;
+// LDS for up to kNear of them, in the plan beyond; the pages it takes for up to kList of them.
+constexpr int kNear = 1024, kList = 4096;
 // Table entries of a fork call that one workgroup of 1024 threads copies by itself: 6.2 us
 // for 32 x 73 entries against 7.6 us in two launches, 7.7 against 8.0 us for 64 x 46.
 constexpr int kSmallTables = 4096;
 
 // Exclusive prefix of x over the workgroup (NT threads), and the total.
-template <int NT>
-__device__ __forceinline__ int block_scan(int x, int* total, int* red) {
+template <int NT, typename T>
+__device__ __forceinline__ T block_scan(T x, T* total, T* red) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int s = x;
+    T s = x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(s, o);
+        const T y = __shfl_up(s, o);
         if (lane >= o) s += y;
     }
     __syncthreads();                       // red may still be read from the scan before
     if (lane == 63) red[wave] = s;
     __syncthreads();
-    int before = 0, all = 0;
+    T before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-        const int y = red[w];
+        const T y = red[w];
         before += w < wave ? y : 0;
         all += y;
     }
@@ -46,29 +46,40 @@ __device__ __forceinline__ int block_scan(int x, int* total, int* red) {
     return before + s - x;
 }
 
+template <int NT>
 struct PlanShared {
-    int need[OCCAM_MAX_BATCH + 1];         // a prefix over the call's sequences
+    static constexpr int kSeqs = NT == 256 ? 256 : OCCAM_MAX_BATCH;
+    long long red2[NT / 64];
+    int need[kSeqs + 1], items[kSeqs + 1]; // prefixes over the call's sequences
     unsigned seen[OCCAM_MAX_SLOTS / 32];   // slots of the call
-    int near[4][kNear];
-    int list[kNear];                       // pages taken, by rank
-    int red[16];
     int bad;
+    int near[4][kSeqs < kNear ? kSeqs : kNear];
+    int list[kList];                       // pages taken, by rank
+    int red[NT / 64];
 };
-static_assert(sizeof(PlanShared) <= 65536, "plan state exceeds the default LDS limit");
 
-// Prefix of the values that get(i) gives for i in [0, n) into out[0 .. n].
+// Prefixes of the two numbers that get(i) gives for i in [0, n) into out[0 .. n] each;
+// returns their sums.  (Sums stay below 2^31: a call's rows do.)
+struct Two { int a, b; };
 template <int NT, typename F>
-__device__ __forceinline__ int prefix_of(int n, int* out, int* red, F get) {
-    int base = 0;
+__device__ __forceinline__ Two prefix_of(int n, int* out_a, int* out_b, long long* red, F get) {
+    long long base = 0;
     for (int i0 = 0; i0 < n; i0 += NT) {
         const int i = i0 + threadIdx.x;
-        int total;
-        const int at = block_scan<NT>(i < n ? get(i) : 0, &total, red);
-        if (i < n) out[i] = base + at;
+        long long total;
+        const Two x = i < n ? get(i) : Two{0, 0};
+        const long long at = base + block_scan<NT>((long long)x.a << 32 | (unsigned)x.b, &total, red);
+        if (i < n) {
+            out_a[i] = (int)(at >> 32);
+            out_b[i] = (int)at;
+        }
         base += total;
     }
-    if (threadIdx.x == 0) out[n] = base;
-    return base;
+    if (threadIdx.x == 0) {
+        out_a[n] = (int)(base >> 32);
+        out_b[n] = (int)base;
+    }
+    return Two{(int)(base >> 32), (int)base};
 }
 
 // The clear bits of word w of the map that are pages.
@@ -85,18 +96,17 @@ __device__ __forceinline__ unsigned first_word(const PageView& p) {
 }
 
 // Takes the lowest `need` free pages, or none if there are not as many (false, in every
-// thread); give(r, page) places the one of rank r.  list: room for `need` of them.
-template <int NT, typename F>
-__device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int need, int* red, int* list,
-                                          F give) {
+// thread), and lists them by rank in list[0 .. need), which the caller may read after a barrier.
+template <int NT>
+__device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int need, int* red, int* list) {
     if (need == 0) return true;
     const int words = (p.num_pages + 31) / 32;
-    int total, rank = block_scan<NT>(__popc(free_bits(p, threadIdx.x, word0)), &total, red);
+    int total, rank = block_scan<NT, int>(__popc(free_bits(p, threadIdx.x, word0)), &total, red);
     const int total0 = total;
     int have = total0;
     for (int w0 = NT; w0 < words && have < need; w0 += NT) {
         const int w = w0 + threadIdx.x;
-        block_scan<NT>(__popc(free_bits(p, w, w < words ? p.taken[w] : ~0u)), &total, red);
+        block_scan<NT, int>(__popc(free_bits(p, w, w < words ? p.taken[w] : ~0u)), &total, red);
         have += total;
     }
     if (have < need) return false;
@@ -117,15 +127,9 @@ __device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int
     for (int w0 = NT; w0 < words && base < need; w0 += NT) {
         const int w = w0 + threadIdx.x;
         const unsigned was = w < words ? p.taken[w] : ~0u;
-        rank = base + block_scan<NT>(__popc(free_bits(p, w, was)), &total, red);
+        rank = base + block_scan<NT, int>(__popc(free_bits(p, w, was)), &total, red);
         take(w, was, rank);
         base += total;
-    }
-    __syncthreads();
-    for (int r = threadIdx.x; r < need; r += NT) {
-        const int page = list[r];
-        p.refs[page] = 1;
-        give(r, page);
     }
     return true;
 }
@@ -140,9 +144,9 @@ __device__ __forceinline__ bool bad_slot(const PageView& p, unsigned* seen, int 
     return (atomicOr(&seen[s >> 5], 1u << (s & 31)) >> (s & 31)) & 1;
 }
 template <int NT>
-__device__ __forceinline__ void begin_call(const PageView& p, PlanShared* sh) {
-    for (int w = threadIdx.x; w < (p.num_seqs + 31) / 32; w += NT) sh->seen[w] = 0;
-    if (threadIdx.x == 0) sh->bad = 0;
+__device__ __forceinline__ void begin_call(const PageView& p, unsigned* seen, int* bad) {
+    for (int w = threadIdx.x; w < (p.num_seqs + 31) / 32; w += NT) seen[w] = 0;
+    if (threadIdx.x == 0) *bad = 0;
     __syncthreads();
 }
 __device__ __forceinline__ void write_header(int* plan, int kind, int n, int items) {
@@ -158,7 +162,8 @@ __global__ __launch_bounds__(256) void pages_reset(PageView p) {
 
 template <int NT>
 __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int* plan) {
-    __shared__ PlanShared sh;
+    extern __shared__ __align__(16) unsigned char lds[];
+    PlanShared<NT>& sh = *reinterpret_cast<PlanShared<NT>*>(lds);
     const int n = b.n, G = 1 << p.shift;
     const unsigned word0 = first_word<NT>(p);
     int* g_first = plan_array(plan, n, PL_FIRST);
@@ -170,7 +175,7 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
     int* tail = near ? sh.near[1] : g_tail;
     int* rows = near ? sh.near[2] : g_rows;
     int* slot = near ? sh.near[3] : g_slot;
-    begin_call<NT>(p, &sh);
+    begin_call<NT>(p, sh.seen, &sh.bad);
     for (int i = threadIdx.x; i < n; i += NT) {
         const int s = slot_of(b, i), r = row_count(b, i);
         int bad = 0, len = 0, src = -1;
@@ -189,48 +194,42 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
     }
     __syncthreads();
     // The pages wanted: those behind the present last one, and one in the place of a shared
-    // partly filled one.
-    const int need = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
+    // partly filled one; and the pages that receive rows.
+    const Two sums = prefix_of<NT>(n, sh.need, sh.items, sh.red2, [&](int i) {
         const int len = first[i], r = rows[i];
-        const int more = ((len + r + G - 1) >> p.shift) - ((len + G - 1) >> p.shift);
-        return more + (tail[i] >= 0 && p.refs[tail[i]] > 1);
+        const int end = (len + r + G - 1) >> p.shift;
+        return Two{end - ((len + G - 1) >> p.shift) + (tail[i] >= 0 && p.refs[tail[i]] > 1),
+                   r > 0 ? end - (len >> p.shift) : 0};
     });
+    const int need = sums.a, total = sums.b;
     __syncthreads();
-    int* list = need <= kNear ? sh.list : plan_record(plan, n, p.max_pages, 0);
-    // A shared last page is replaced by the first page its sequence gets: table entry
-    // len / G; otherwise the first one goes behind, at ceil(len / G).
-    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
-            const int i = owner_of(sh.need, n, r), len = first[i];
-            const int wanted = sh.need[i + 1] - sh.need[i];
-            const int pages = (len + rows[i] + G - 1) >> p.shift;
-            const int j = pages - wanted + (r - sh.need[i]);
-            p.table[(size_t)slot[i] * p.max_pages + j] = page;
-        })) {
+    const bool listed = need <= kList;
+    int* list = listed ? sh.list : plan_record(plan, n, p.max_pages, 0);
+    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list)) {
         if (threadIdx.x == 0) {
             atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
             write_header(plan, kPlanReserve, n, 0);
         }
         return;
     }
-    // Only after the taking: a page given up here is not one of those just taken.
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += NT) {
-        if (rows[i] == 0) continue;
-        p.length[slot[i]] = first[i] + rows[i];
-        // One page more than lies behind: the shared tail was replaced.
-        const int more = ((first[i] + rows[i] + G - 1) >> p.shift) - ((first[i] + G - 1) >> p.shift);
-        if (sh.need[i + 1] - sh.need[i] > more) drop_ref(p, tail[i]);
+    // The first table entry that sequence i gets: a shared last page is replaced by the first
+    // page taken (entry len / G); otherwise that one goes behind, at ceil(len / G).
+    auto fresh_from = [&](int i) {
+        return ((first[i] + rows[i] + G - 1) >> p.shift) - (sh.need[i + 1] - sh.need[i]);
+    };
+    for (int r = threadIdx.x; r < need; r += NT) {
+        const int i = owner_of(sh.need, n, r), page = list[r];
+        p.refs[page] = 1;
+        p.table[(size_t)slot[i] * p.max_pages + fresh_from(i) + r - sh.need[i]] = page;
     }
-    __syncthreads();
-    const int total = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
-        const int len = first[i], r = rows[i];
-        return r > 0 ? ((len + r + G - 1) >> p.shift) - (len >> p.shift) : 0;
-    });
-    __syncthreads();
+    if (!listed) __syncthreads();          // the list lies where the records go
     for (int x = threadIdx.x; x < total; x += NT) {
-        const int i = owner_of(sh.need, n, x), len = first[i];
-        const int j = (len >> p.shift) + x - sh.need[i], pos0 = j << p.shift;
-        const int page = p.table[(size_t)slot[i] * p.max_pages + j];
+        const int i = owner_of(sh.items, n, x), len = first[i];
+        const int j = (len >> p.shift) + x - sh.items[i], pos0 = j << p.shift, from = fresh_from(i);
+        const int page = j < from ? tail[i]
+                         : listed ? list[sh.need[i] + j - from]
+                                  : p.table[(size_t)slot[i] * p.max_pages + j];
         const int had = len > pos0 ? len - pos0 : 0, now = len + rows[i] - pos0;
         int* r = plan_record(plan, n, p.max_pages, x);
         r[RR_PAGE] = page;
@@ -238,6 +237,14 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
         r[RR_HAD] = had;
         r[RR_END] = now < G ? now : G;
         r[RR_ROW] = row_begin(b, i) - len + pos0;
+    }
+    // References end after the taking: a page given up here is not one of those just taken.
+    for (int i = threadIdx.x; i < n; i += NT) {
+        if (rows[i] == 0) continue;
+        p.length[slot[i]] = first[i] + rows[i];
+        // One page more than lies behind: the shared tail was replaced.
+        const int more = ((first[i] + rows[i] + G - 1) >> p.shift) - ((first[i] + G - 1) >> p.shift);
+        if (sh.need[i + 1] - sh.need[i] > more) drop_ref(p, tail[i]);
     }
     if (threadIdx.x == 0) write_header(plan, kPlanReserve, n, total);
 }
@@ -247,23 +254,24 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
 template <int NT, bool COPY>
 __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* src, const int* dst,
                                                 int* plan) {
-    __shared__ PlanShared sh;
+    __shared__ unsigned seen[OCCAM_MAX_SLOTS / 32];
+    __shared__ int bad;
     int* lens = plan_array(plan, n, PL_LENS);
-    begin_call<NT>(p, &sh);
+    begin_call<NT>(p, seen, &bad);
     for (int i = threadIdx.x; i < n; i += NT) {
         const int s = src[i], t = dst[i];
         int len = 0;
-        if (bad_slot(p, sh.seen, t) || s < 0 || s >= p.num_seqs || p.length[t] != 0) sh.bad = 1;
+        if (bad_slot(p, seen, t) || s < 0 || s >= p.num_seqs || p.length[t] != 0) bad = 1;
         else len = p.length[s];
         lens[i] = len;
     }
     __syncthreads();
-    if (sh.bad) {
+    if (bad) {
         for (int i = threadIdx.x; i < n; i += NT) lens[i] = -1;
         if (threadIdx.x == 0) atomicOr(p.status, (int)OCCAM_PAGES_BAD_SEQ);
     }
     if (threadIdx.x == 0) write_header(plan, kPlanFork, n, 0);
-    if (!COPY || sh.bad) return;
+    if (!COPY || bad) return;
     for (int x = threadIdx.x; x < n * p.max_pages; x += NT) {
         const int i = x / p.max_pages, j = x - i * p.max_pages, len = lens[i];
         if (j >= (len + (1 << p.shift) - 1) >> p.shift) continue;
@@ -306,9 +314,20 @@ __global__ __launch_bounds__(256) void pages_free(PageView p, const int* seq) {
 }
 
 // The first of m ascending distinct indices that is not its own position (m if none): the
-// first token dropped.  Seven probes a round, side by side.
+// first token dropped.  Probes side by side: at first 0, 1, 3, 7, ... (a pruned span has its
+// first gap early), then seven a round.
 __device__ __forceinline__ int first_gap(const int* idx, int m) {
     int lo = 0, hi = m;                        // idx[lo - 1] == lo - 1; idx[hi] != hi or hi == m
+    {
+        constexpr int K = 14;
+        int at[K], good = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) at[k] = (1 << k) - 1 < m ? idx[(1 << k) - 1] - ((1 << k) - 1) : 1;
+#pragma unroll
+        for (int k = 0; k < K; ++k) good += at[k] == 0 && good == k;
+        lo = good ? 1 << (good - 1) : 0;
+        if (good < K && (1 << good) - 1 < hi) hi = (1 << good) - 1;
+    }
     while (hi - lo > 0) {
         const int step = (hi - lo + 7) >> 3;
         int at[7], good = 0;
@@ -333,7 +352,8 @@ template <int NT>
 __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* seq, const int* start,
                                                 const int* span, const int* idx, const int* off,
                                                 int* plan) {
-    __shared__ PlanShared sh;
+    extern __shared__ __align__(16) unsigned char lds[];
+    PlanShared<NT>& sh = *reinterpret_cast<PlanShared<NT>*>(lds);
     const int G = 1 << p.shift;
     const unsigned word0 = first_word<NT>(p);
     int* g_first = plan_array(plan, n, PL_FIRST);
@@ -343,7 +363,7 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
     int* first = near ? sh.near[0] : g_first;
     int* olds = near ? sh.near[1] : g_olds;
     int* news = near ? sh.near[2] : g_news;
-    begin_call<NT>(p, &sh);
+    begin_call<NT>(p, sh.seen, &sh.bad);
     for (int i = threadIdx.x; i < n; i += NT) {
         const int s = seq[i], a = start[i], m = span[i], o = off[i], c = off[i + 1] - o;
         int bad = 0, len = 0, now = 0, f = 0;
@@ -366,16 +386,14 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
-    const int need = prefix_of<NT>(n, sh.need, sh.red, [&](int i) {
+    const int need = prefix_of<NT>(n, sh.need, sh.items, sh.red2, [&](int i) {
         const int pages = ((news[i] + G - 1) >> p.shift) - first[i];
-        return sh.bad || pages < 0 ? 0 : pages;
-    });
+        return Two{sh.bad || pages < 0 ? 0 : pages, 0};
+    }).a;
     __syncthreads();
-    int* list = need <= kNear ? sh.list : plan_record(plan, n, p.max_pages, 0);
-    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list, [&](int r, int page) {
-            const int i = owner_of(sh.need, n, r);
-            plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
-        })) {
+    const bool listed = need <= kList;
+    int* list = listed ? sh.list : plan_record(plan, n, p.max_pages, 0);
+    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list)) {
         for (int i = threadIdx.x; i < n; i += NT) {
             g_news[i] = olds[i];
             g_first[i] = (olds[i] + G - 1) >> p.shift;
@@ -386,12 +404,18 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         }
         return;
     }
-    __syncthreads();                       // the list may lie where the records go
+    __syncthreads();
+    for (int r = threadIdx.x; r < need; r += NT) {
+        const int i = owner_of(sh.need, n, r), page = list[r];
+        p.refs[page] = 1;
+        plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
+    }
+    if (!listed) __syncthreads();          // the list lies where the records go
     for (int x = threadIdx.x; x < need; x += NT) {
         const int i = owner_of(sh.need, n, x), j = first[i] + x - sh.need[i];
         const int now = news[i] - (j << p.shift);
         int* r = plan_record(plan, n, p.max_pages, x);
-        r[RK_PAGE] = plan_pages(plan, n, p.max_pages, i)[j];
+        r[RK_PAGE] = listed ? list[x] : plan_pages(plan, n, p.max_pages, i)[j];
         r[RK_POS] = j << p.shift;
         r[RK_END] = now < G ? now : G;
         r[RK_SEQ] = i;
@@ -430,9 +454,19 @@ hipError_t launch_pages_reset(const PageView& p, hipStream_t s) {
     return launch(pages_reset, dim3((most + 255) / 256), dim3(256), 0, s, p);
 }
 
+// A planning kernel with its state in LDS.
+template <int NT, auto kernel, typename... A>
+static hipError_t plan_launch(hipStream_t s, A... args) {
+    constexpr int bytes = sizeof(PlanShared<NT>);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = bytes <= 65536 ? hipSuccess
+                                        : allow_lds(reinterpret_cast<const void*>(kernel), bytes, done);
+    return e != hipSuccess ? e : launch(kernel, dim3(1), dim3(NT), bytes, s, args...);
+}
+
 hipError_t launch_pages_reserve(const PageView& p, const BatchView& b, int* plan, hipStream_t s) {
-    return b.n <= 256 ? launch(pages_reserve<256>, dim3(1), dim3(256), 0, s, p, b, plan)
-                      : launch(pages_reserve<1024>, dim3(1), dim3(1024), 0, s, p, b, plan);
+    return b.n <= 256 ? plan_launch<256, pages_reserve<256>>(s, p, b, plan)
+                      : plan_launch<1024, pages_reserve<1024>>(s, p, b, plan);
 }
 
 hipError_t launch_pages_fork(const PageView& p, int n, const int* src, const int* dst, int* plan,
@@ -454,8 +488,8 @@ hipError_t launch_pages_keep(const PageView& p, int n, const int* seq, const int
                              const int* span, const int* idx, const int* off, int* plan,
                              hipStream_t s) {
     hipError_t e = n <= 256
-        ? launch(keep_plan<256>, dim3(1), dim3(256), 0, s, p, n, seq, start, span, idx, off, plan)
-        : launch(keep_plan<1024>, dim3(1), dim3(1024), 0, s, p, n, seq, start, span, idx, off, plan);
+        ? plan_launch<256, keep_plan<256>>(s, p, n, seq, start, span, idx, off, plan)
+        : plan_launch<1024, keep_plan<1024>>(s, p, n, seq, start, span, idx, off, plan);
     if (e != hipSuccess) return e;
     return launch(keep_swap, dim3(n), dim3(256), 0, s, p, n, seq, plan);
 }
