@@ -424,15 +424,23 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
 // products).  The running maximum only moves the sums when some row's maximum passed the
 // one in use by more than 2^8: probabilities are held times 2^6, so they stay below 2^14.
 //
-// Work alternates between matrix phases (the scores of tile t, the output of tile t - 1) and
-// vector phases (the softmax of tile t, the conversion of a tile to come), a barrier after
-// each.  With eight waves, the second four run one phase behind, so that of the two waves
-// of a SIMD one feeds the matrix core while the other does vector work.  The tile written
-// in vector phase t is t + AHEAD: with phases A: M(t) = 2t, V(t) = 2t + 1 and B: one later,
-// keys t are read until phase 2t + 1 and values t until 2t + 3, and the last share of tile
-// t is written in B's V(t - 2) = 2t - 2; four buffers keep every write past the last read of
-// the tile before (2 (t - 4) + 3 < 2 (t - 2) + 1).  One group needs one tile ahead and two
-// buffers.
+// A wave alternates between a vector phase (the softmax of tile t) and a matrix phase (the
+// output of tile t, the scores of t + 1).  With eight waves, the two of a SIMD belong to two
+// groups, B a phase behind A, so that one feeds the matrix core while the other does vector
+// work.  There is one barrier per tile: behind the matrix phase for A, before it for B.
+// Between two barriers (step t) A reads values t and keys t + 1, B values t - 1 and keys t,
+// and both store their share of tile t + 2 (beside their products, whose issue slots leave
+// room), so four buffers are enough: tile t + 2 takes the place of t - 2, whose values B read
+// last in step t - 1.  The codes of two further tiles are on their way from memory.
+// (A barrier behind every phase: 337 us for the prompt below, against 328.)
+// With four waves (dp = 64 and 256: other waves of a CU are other workgroups) a tile is stored
+// in the vector phase before its matrix phase, with a barrier behind each and two buffers.
+//
+// What bounds it is the issue of vector instructions beside the matrix core: the products of
+// a tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about
+// as many.  A causal prompt of 4 x 3012 tokens, 32 heads of 128: 328 us, 906 TFLOP/s (a large
+// bf16 matrix product reaches 1342 here); text rows of 32 images, 16 to 512 of them over 272
+// to 4608 tokens: 248 us, 895 TFLOP/s.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
@@ -489,7 +497,11 @@ __global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entr
 
 template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
 template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
-template <int DP> constexpr int many_lds() { return many_bufs<DP>() * 2 * kTile * DP * 2; }
+// A buffer: keys [64] of 2 DP + 16 bytes, so that 16 rows' reads of 16 bytes fall on all
+// banks; values [tile of 32][16 tokens][half][DP][8 tokens], the 8 reduction slots of a lane.
+template <int DP> constexpr int many_keys() { return kTile * (DP * 2 + 16); }
+template <int DP> constexpr int many_buf() { return many_keys<DP>() + kTile * DP * 2; }
+template <int DP> constexpr int many_lds() { return many_bufs<DP>() * many_buf<DP>(); }
 
 template <int DP>
 __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
@@ -503,10 +515,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     constexpr int UV = kTile * DP / 16 / THREADS;    // value units (2 elements x 8 tokens)
     static_assert(UK * THREADS * 16 == kTile * DP, "tile units");
     extern __shared__ __align__(16) unsigned char lds[];
-    // [buffer][keys | values]: keys [64][DP] bf16, 16-byte chunk c of row m in slot
-    // c ^ (m % 16) (16 rows' reads of one chunk fall on all banks); values
-    // [tile of 32][16 tokens][half][DP][8 tokens] f16, the 8 reduction slots of a lane.
-    constexpr int HALF = kTile * DP * 2;
+    constexpr int KP = DP * 2 + 16, HALF = many_keys<DP>(), BUF = many_buf<DP>();
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 31, half = lane >> 5;
     // A workgroup per part of a row block; every sequence's last row block first.
@@ -598,14 +607,12 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         }
     };
     // Where this thread's units go, relative to the buffer.
-    unsigned kto[UK][2], vto[UV];
+    unsigned kto[UK], vto[UV];
 #pragma unroll
     for (int u = 0; u < UK; ++u) {
         const int unit = u * THREADS + threadIdx.x;
         const int mrow = unit / (DP / 16), c = (unit - mrow * (DP / 16)) * 2;
-        const int swz = mrow & (CH < 16 ? CH - 1 : 15);
-        kto[u][0] = mrow * DP * 2 + (c ^ swz) * 16;
-        kto[u][1] = mrow * DP * 2 + ((c + 1) ^ swz) * 16;
+        kto[u] = mrow * KP + c * 16;
         vto[u] = HALF + unit * 32;
     }
     auto mask_tile = [&](int pos, Raw& r) {
@@ -624,9 +631,9 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     };
     // Part x of four, of unit u.
     auto store_part = [&](const Raw& r, int buf, int to, int u, int x) {
-        unsigned char* d = lds + buf * 2 * HALF;
+        unsigned char* d = lds + buf * BUF;
         if (x < 2) {
-            *reinterpret_cast<bf16x8*>(d + kto[u][x]) = codes_bf16(r.k[u][x * 2], r.k[u][x * 2 + 1], r.sk[u]);
+            *reinterpret_cast<bf16x8*>(d + kto[u] + x * 16) = codes_bf16(r.k[u][x * 2], r.k[u][x * 2 + 1], r.sk[u]);
         } else {
             const float sc = exp_scale(r.sv[u] - to < -126 ? -126 : r.sv[u] - to);
             *reinterpret_cast<f16x8*>(d + vto[u] + (x - 2) * 16) =
@@ -641,19 +648,18 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     };
     f32x16 s[2];
     f16x8 p[4];
-    const int sw = n & (CH < 16 ? CH - 1 : 15);
     // The output of the tile in buffer `out` (values times p) and the scores of the one in
     // `in`, one product after the other; more(i) is other work for after product i.
     constexpr int OUT = 4 * ND, PRODUCTS = OUT + 2 * NK;
     auto matrix = [&](auto first, int out, int in, auto&& more) {
         constexpr int FIRST = decltype(first)::value;
-        const unsigned char* kd = lds + in * 2 * HALF + n * DP * 2;
-        const unsigned char* vd = lds + out * 2 * HALF + HALF + (half * DP + n) * 16;
+        const unsigned char* kd = lds + in * BUF + n * KP + half * 16;
+        const unsigned char* vd = lds + out * BUF + HALF + (half * DP + n) * 16;
         u32x4 f[kReads];
         auto operand = [&](int i) {
             if (i < OUT) return *reinterpret_cast<const u32x4*>(vd + (i / ND) * 2 * DP * 16 + (i % ND) * 512);
             const int c = (i - OUT) / 2, u = (i - OUT) % 2;
-            return *reinterpret_cast<const u32x4*>(kd + u * 32 * DP * 2 + ((c * 2 + half) ^ sw) * 16);
+            return *reinterpret_cast<const u32x4*>(kd + u * 32 * KP + c * 32);
         };
 #pragma unroll
         for (int i = FIRST; i < FIRST + kReads; ++i) f[i % kReads] = operand(i);
@@ -737,7 +743,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
             if (in == 32) win_scales(base + 64, nxt);
         };
         auto fetch = [&](int tile, Raw& r) { load_tile(tile, win, r); };
-        int refs[AHEAD + 1];                     // of tiles t .. t + AHEAD
+        int refs[3];                             // of the tiles from the present one on
         int to = kMinExp;
         Raw start[AHEAD];
 #pragma unroll
@@ -747,7 +753,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         // Queries: whole rows from memory, after the tiles (loads return in order), turned
         // into operands through the buffers that no tile is stored to yet.
         constexpr int RPI = 64 / CH;                               // rows per instruction
-        static_assert(WAVES * 32 * DP * 2 <= (BUFS - AHEAD) * 2 * HALF, "queries in the free buffers");
+        static_assert(WAVES * 32 * DP * 2 <= (BUFS - AHEAD) * BUF, "queries in the free buffers");
         // Rows behind the last one read the sequence's first row; nothing of theirs is written.
         const long long from = live ? orow * a.q_stride + (long long)hh * a.c.d
                                     : (long long)row_begin(a.b, i) * a.q_stride + (long long)h * a.g * a.c.d;
@@ -766,64 +772,87 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
             store_tile(start[x], x % BUFS, to);
             refs[x] = to;
         }
-        unsigned char* qd = lds + AHEAD * 2 * HALF + wave * 32 * DP * 2;
+        // (16-byte chunk c of row r in slot c ^ (r % 16).)
+        constexpr int SW = CH < 16 ? CH - 1 : 15;
+        unsigned char* qd = lds + AHEAD * BUF + wave * 32 * DP * 2;
 #pragma unroll
         for (int x = 0; x < 32 / RPI; ++x) {
             const int r = x * RPI + lane / CH;
             if (!inside) qx[x] = u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4*>(qd + r * DP * 2 + (chunk ^ (r & (CH < 16 ? CH - 1 : 15))) * 16) = qx[x];
+            *reinterpret_cast<u32x4*>(qd + r * DP * 2 + (chunk ^ (r & SW)) * 16) = qx[x];
         }
 #pragma unroll
         for (int c = 0; c < NK; ++c)
-            q[c] = *reinterpret_cast<const bf16x8*>(qd + n * DP * 2 + ((c * 2 + half) ^ sw) * 16);
+            q[c] = *reinterpret_cast<const bf16x8*>(qd + n * DP * 2 + ((c * 2 + half) ^ (n & SW)) * 16);
         lds_barrier();
-        const bool behind = AHEAD == 2 && wave >= 4;
-        if (behind) lds_barrier();
         const auto nothing = [](int) {};
         const std::integral_constant<int, 0> all;
-        matrix(std::integral_constant<int, OUT>{}, 0, 0, nothing);
-        lds_barrier();
-        // One tile: `r` holds tile + AHEAD, and tile + AHEAD + SETS afterwards.
-        auto step = [&](int tile, Raw& r) {
-            const int pos = lo + tile * kTile, to_store = (tile + AHEAD) % BUFS;
-            if (pos < wave_hi) softmax(pos, refs[0]);
-            if (AHEAD == 1) {
-                mask_tile(pos + kTile, r);
-                to = r.top > to ? r.top : to;
-                store_tile(r, to_store, to);
-                window(tile + 1 + SETS);
-                fetch(tile + 1 + SETS, r);
-            }
+        const std::integral_constant<int, OUT> scores;
+        if constexpr (AHEAD == 1) {
+            matrix(scores, 0, 0, nothing);
             lds_barrier();
-            // (After the last tile the scores are of a stale one and unused.)
-            if (AHEAD == 1) {
+            for (int tile = 0; tile < tiles; ++tile) {
+                const int pos = lo + tile * kTile;
+                if (pos < wave_hi) softmax(pos, refs[0]);
+                mask_tile(pos + kTile, raw[0]);
+                to = raw[0].top > to ? raw[0].top : to;
+                store_tile(raw[0], (tile + 1) % BUFS, to);
+                window(tile + 1 + SETS);
+                fetch(tile + 1 + SETS, raw[0]);
+                lds_barrier();
+                // (After the last tile the scores are of a stale one and unused.)
                 if (pos < wave_hi) matrix(all, tile % BUFS, (tile + 1) % BUFS, nothing);
-            } else {
-                __builtin_amdgcn_s_setprio(1);
-                mask_tile(pos + 2 * kTile, r);
-                window(tile + 2 + SETS);
+                refs[0] = to;
+                lds_barrier();
+            }
+        } else {
+            const int behind = wave >= 4;
+            // What a matrix phase does beside its products: tile x from `r` to LDS, and what
+            // comes after it into `r`.
+            auto coming = [&](int x, Raw& r) {
+                mask_tile(lo + x * kTile, r);
+                window(x + SETS);
                 to = r.top > to ? r.top : to;
+            };
+            auto beside = [&](int i, int x, Raw& r) {
+                if (i % 2 == 0 && i < 8) store_part(r, x % BUFS, to, 0, i / 2);
+                if (i == 9) fetch(x + SETS, r);
+            };
+            if (behind) {
+                coming(2, raw[0]);
+                matrix(scores, 0, 0, [&](int i) { beside(i - OUT, 2, raw[0]); });
+                refs[2] = to;
+                const Raw r = raw[0];
+                raw[0] = raw[1];
+                raw[1] = r;
+            } else {
+                matrix(scores, 0, 0, nothing);
+            }
+            // One tile: `r` holds the one that is stored beside its output.
+            auto step = [&](int tile, Raw& r) {
+                const int pos = lo + tile * kTile, x = tile + 2 + behind;
+                if (pos < wave_hi) softmax(pos, refs[0]);
+                if (behind) lds_barrier();
+                __builtin_amdgcn_s_setprio(1);
+                coming(x, r);
                 if (pos < wave_hi) {
-                    matrix(all, tile % BUFS, (tile + 1) % BUFS, [&](int i) {
-                        if (i % 2 == 0 && i < 8) store_part(r, to_store, to, 0, i / 2);
-                        if (i == 9) fetch(tile + 2 + SETS, r);
-                    });
+                    matrix(all, tile % BUFS, (tile + 1) % BUFS, [&](int i) { beside(i, x, r); });
                 } else {
-                    store_tile(r, to_store, to);
-                    fetch(tile + 2 + SETS, r);
+                    store_tile(r, x % BUFS, to);
+                    fetch(x + SETS, r);
                 }
                 __builtin_amdgcn_s_setprio(0);
+                refs[0] = refs[1];
+                refs[1] = behind ? refs[2] : to;
+                refs[2] = to;
+                if (!behind) lds_barrier();
+            };
+            for (int tile = 0; tile < tiles; tile += SETS) {
+                step(tile, raw[0]);
+                if (tile + 1 < tiles) step(tile + 1, raw[SETS - 1]);
             }
-#pragma unroll
-            for (int x = 0; x + 1 < AHEAD; ++x) refs[x] = refs[x + 1];
-            refs[AHEAD - 1] = to;
-            lds_barrier();
-        };
-        for (int tile = 0; tile < tiles; tile += SETS) {
-            step(tile, raw[0]);
-            if (SETS == 2 && tile + 1 < tiles) step(tile + 1, raw[SETS - 1]);
+            lds_barrier();                       // the last tile has been read by everyone
         }
-        if (AHEAD == 2 && !behind) lds_barrier();
     }
     l += __shfl_xor(l, 32);
     const float inv = l > 0.f ? 1.f / l : 0.f;
