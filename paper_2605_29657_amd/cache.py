@@ -114,9 +114,10 @@ _current = torch._C._cuda_getDevice
 _heads = struct.Struct("PPi4xqq").pack          # an occam_heads
 
 
-def _enqueue(fn, device, stream, *args):
-    """Call ``fn(*args, stream)`` with ``device`` current and raise on an error status."""
-    index = device.index
+# Devices are compared by index (a tensor elsewhere than on a GPU has -1): what a call costs
+# on the host is much of what a small one costs at all.
+def _enqueue(fn, index, stream, *args):
+    """Call ``fn(*args, stream)`` with device ``index`` current and raise on an error status."""
     if stream is None:
         stream = _raw_stream(index)
     elif isinstance(stream, torch.cuda.Stream):
@@ -124,7 +125,7 @@ def _enqueue(fn, device, stream, *args):
     if index == _current():
         st = fn(*args, stream)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             st = fn(*args, stream)
     if st:
         raise occam.OccamError(st, occam.status_string(st))
@@ -137,22 +138,26 @@ def _bad(msg):
 _I32, _F32 = torch.int32, torch.float32
 
 
-def _ints(t, device, name, at_least=0):
+def _ints(t, index, name, at_least=0):
     """Pointer of an int32 device vector (None stays None)."""
     if t is None:
         return None
-    if t.dtype is not _I32 or t.device != device or not t.is_contiguous() or t.numel() < at_least:
-        _bad("%s must be a contiguous int32 tensor on %s with at least %d elements" % (name, device, at_least))
+    if t.dtype is not _I32 or t.get_device() != index or not t.is_contiguous() or (
+            at_least and t.numel() < at_least):
+        _bad("%s must be a contiguous int32 tensor on GPU %s with at least %d elements" % (name, index, at_least))
     return t.data_ptr()
 
 
-def _rows(t, device, name, heads, dim, dtype):
-    """(pointer, row stride) of a tensor [rows, heads, dim] whose heads are packed."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 3 and shape[1] == heads and shape[2] == dim and t.dtype is dtype and t.device == device:
-        if not shape[0] or ((stride[2] == 1 or dim == 1) and (stride[1] == dim or heads == 1)):
-            return t.data_ptr(), (stride[0] if shape[0] > 1 else heads * dim)
-    _bad("%s must be a [rows, %d, %d] tensor of %s on %s with packed heads" % (name, heads, dim, dtype, device))
+def _rows(t, index, name, heads, dim, dtype):
+    """(pointer, row stride, rows) of a tensor [rows, heads, dim] whose heads are packed."""
+    shape = t.shape
+    if len(shape) == 3 and t.dtype is dtype and t.get_device() == index:
+        n, h, w = shape
+        if h == heads and w == dim:
+            s0, s1, s2 = t.stride()
+            if not n or ((s2 == 1 or dim == 1) and (s1 == dim or heads == 1)):
+                return t.data_ptr(), (s0 if n > 1 else heads * dim), n
+    _bad("%s must be a [rows, %d, %d] tensor of %s on GPU %s with packed heads" % (name, heads, dim, dtype, index))
 
 
 _DTYPES = {torch.float32: occam.F32, torch.bfloat16: occam.BF16}
@@ -195,22 +200,21 @@ def rotate(rotary, positions, src, dst=None, inverse=False, stream=None):
     dst = src if dst is None else dst
     if not src or len(src) != len(dst) or len(src) > occam.MAX_ROW_TENSORS:
         _bad("src and dst must be lists of 1 to %d tensors" % occam.MAX_ROW_TENSORS)
-    x = src[0]
-    dev, dt, rows, d = x.device, x.dtype, x.shape[0], rotary.head_dim
-    if dt not in _DTYPES or dev.type != "cuda" or positions.numel() != rows * rotary.axes:
+    x, d = src[0], rotary.head_dim
+    index, dt, rows = x.get_device(), x.dtype, x.shape[0] if x.dim() else 0
+    if dt not in _DTYPES or index < 0 or positions.numel() != rows * rotary.axes:
         _bad("positions must have %d axes for every row, tensors float32 or bfloat16 on a GPU" % rotary.axes)
     heads = b""
     for t, o in zip(src, dst):
-        if t.dim() != 3 or t.shape[0] != rows or o.shape != t.shape:
+        n = t.shape[1] if t.dim() == 3 else 0
+        ps, ss, r = _rows(t, index, "src", n, d, dt)
+        pd, sd, q = (ps, ss, r) if o is t else _rows(o, index, "dst", n, d, dt)
+        if r != rows or q != rows:
             _bad("every tensor must have the same rows")
-        n = t.shape[1]
-        ps, ss = pd, sd = _rows(t, dev, "src", n, d, dt)
-        if o is not t:
-            pd, sd = _rows(o, dev, "dst", n, d, dt)
         heads += _heads(ps, pd, n, ss, sd)
     if rows == 0:
         return
-    _enqueue(lib().occam_rotate, dev, stream, rotary.ref, rows, _ints(positions, dev, "positions"),
+    _enqueue(lib().occam_rotate, index, stream, rotary.ref, rows, _ints(positions, index, "positions"),
              1 if inverse else 0, _DTYPES[dt], len(src), heads)
 
 
@@ -225,7 +229,7 @@ class Pages:
             _bad("the pages must be on a GPU")
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
-        self.device = device
+        self.device, self.index = device, device.index
         self.num_pages, self.page_tokens = int(num_pages), int(page_tokens)
         self.num_seqs, self.max_pages = int(num_seqs), int(max_pages)
         self.c = _Pages(self.num_pages, self.page_tokens, self.num_seqs, self.max_pages)
@@ -269,23 +273,21 @@ class Batch:
     def __init__(self, n, rows=1, seq=None, row_offsets=None, max_rows=0):
         self.n, self.seq, self.row_offsets = int(n), seq, row_offsets     # kept alive
         self.rows = int(rows)
-        self.device = None
+        self.index = None
         for t, least, name in ((seq, self.n, "seq"), (row_offsets, self.n + 1, "row_offsets")):
             if t is not None:
-                self.device = t.device if self.device is None else self.device
-                _ints(t, self.device, name, least)
+                self.index = t.get_device() if self.index is None else self.index
+                _ints(t, self.index, name, least)
         self.c = _Batch(self.n, None if seq is None else seq.data_ptr(), self.rows,
                         None if row_offsets is None else row_offsets.data_ptr(), int(max_rows))
         self.ref = ctypes.byref(self.c)
 
-    def check(self, device, *tensors):
-        if self.device is not None and self.device != device:
-            _bad("the batch's tensors must be on %s" % device)
-        if self.row_offsets is None:
-            least = self.n * self.rows
-            for t in tensors:
-                if t is not None and t.shape[0] < least:
-                    _bad("the batch has %d rows, a tensor %d" % (least, t.shape[0]))
+    def check(self, index, rows=None):
+        """The batch's tensors are on GPU ``index``, and tensors of ``rows`` rows hold its rows."""
+        if self.index is not None and self.index != index:
+            _bad("the batch's tensors must be on GPU %s" % index)
+        if rows is not None and self.row_offsets is None and rows < self.n * self.rows:
+            _bad("the batch has %d rows, a tensor %d" % (self.n * self.rows, rows))
 
 
 def plan(pages, n):
@@ -298,33 +300,34 @@ def plan(pages, n):
 
 
 def _plan(pages, p):
-    return _ints(p, pages.device, "plan"), p.numel() * 4
+    return _ints(p, pages.index, "plan"), p.numel() * 4
 
 
 def reset(pages, stream=None):
-    _enqueue(lib().occam_pages_reset, pages.device, stream, pages.ref)
+    _enqueue(lib().occam_pages_reset, pages.index, stream, pages.ref)
 
 
 def reserve(pages, batch, plan, stream=None):
-    batch.check(pages.device)
-    _enqueue(lib().occam_pages_reserve, pages.device, stream, pages.ref, batch.ref, *_plan(pages, plan))
+    batch.check(pages.index)
+    _enqueue(lib().occam_pages_reserve, pages.index, stream, pages.ref, batch.ref, *_plan(pages, plan))
 
 
 def fork(pages, src, dst, plan, stream=None):
-    n = src.numel()
-    _enqueue(lib().occam_pages_fork, pages.device, stream, pages.ref, n,
-             _ints(src, pages.device, "src"), _ints(dst, pages.device, "dst", n), *_plan(pages, plan))
+    n, dev = src.numel(), pages.index
+    _enqueue(lib().occam_pages_fork, dev, stream, pages.ref, n, _ints(src, dev, "src"),
+             _ints(dst, dev, "dst", n), *_plan(pages, plan))
 
 
 def free(pages, seq, stream=None):
-    _enqueue(lib().occam_pages_free, pages.device, stream, pages.ref, seq.numel(),
-             _ints(seq, pages.device, "seq"))
+    dev = pages.index
+    _enqueue(lib().occam_pages_free, dev, stream, pages.ref, seq.numel(), _ints(seq, dev, "seq"))
 
 
 def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=None):
-    n, dev = seq.numel(), pages.device
+    n = seq.numel()
     if kept_offsets.numel() != n + 1:             # move() takes n from it
         _bad("kept_offsets must have %d elements" % (n + 1))
+    dev = pages.index
     _enqueue(lib().occam_pages_keep, dev, stream, pages.ref, n, _ints(seq, dev, "seq"),
              _ints(span_start, dev, "span_start", n), _ints(span_len, dev, "span_len", n),
              _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets"),
@@ -334,37 +337,42 @@ def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=
 # ------------------------------------------------------------------------------- rows
 def append(pages, layer, batch, plan, k, v, stream=None):
     """occam_cache_append: ``k`` and ``v`` [rows, num_kv_heads, head_dim], float32 or bfloat16."""
-    dev = pages.device
-    batch.check(dev, k, v)
-    if k.dtype != v.dtype or k.dtype not in _DTYPES or k.shape[0] != v.shape[0]:
-        _bad("k and v must have the same rows and be both float32 or both bfloat16")
-    kp = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, k.dtype)
-    vp = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, k.dtype)
-    if k.shape[0] == 0:
+    dev, dt = pages.index, k.dtype
+    if dt not in _DTYPES:
+        _bad("k and v must be float32 or bfloat16 tensors")
+    kp, ks, n = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, dt)
+    vp, vs, m = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, dt)
+    if n != m:
+        _bad("k and v must have the same rows")
+    batch.check(dev, n)
+    if n == 0:
         return
     _enqueue(lib().occam_cache_append, dev, stream, pages.ref, layer.ref, batch.ref, *_plan(pages, plan),
-             _DTYPES[k.dtype], *kp, *vp)
+             _DTYPES[dt], kp, ks, vp, vs)
 
 
 def read(pages, layer, batch, k, v=None, start=None, stream=None):
     """occam_cache_read into ``k`` and ``v`` (either may be None), float32 or bfloat16."""
-    dev = pages.device
-    batch.check(dev, k, v)
+    dev = pages.index
     x = k if k is not None else v
     if x is None or x.dtype not in _DTYPES:
         _bad("k or v must be a float32 or bfloat16 tensor")
-    ptrs = []
-    for t, name in ((k, "k"), (v, "v")):
-        ptrs += (None, 0) if t is None else _rows(t, dev, name, layer.num_kv_heads, layer.head_dim, x.dtype)
+    dt, kp, ks, vp, vs = x.dtype, None, 0, None, 0
+    if k is not None:
+        kp, ks, n = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, dt)
+        batch.check(dev, n)
+    if v is not None:
+        vp, vs, n = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, dt)
+        batch.check(dev, n)
     if x.shape[0] == 0:
         return
     _enqueue(lib().occam_cache_read, dev, stream, pages.ref, layer.ref, batch.ref,
-             _ints(start, dev, "start", batch.n), _DTYPES[x.dtype], *ptrs)
+             _ints(start, dev, "start", batch.n), _DTYPES[dt], kp, ks, vp, vs)
 
 
 def move(pages, layer, plan, kept_idx, kept_offsets, stream=None):
     """occam_cache_move with the plan and the lists of :func:`keep`."""
-    dev = pages.device
+    dev = pages.index
     _enqueue(lib().occam_cache_move, dev, stream, pages.ref, layer.ref, kept_offsets.numel() - 1,
              *_plan(pages, plan), _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets"))
 
@@ -387,17 +395,17 @@ def attend(pages, layer, batch, q, out, ws, lse=None, causal=True, softmax_scale
            stream=None):
     """occam_cache_attend: ``q`` and ``out`` bfloat16 [rows, num_heads, head_dim], ``lse``
     float32 [rows, num_heads] or None.  ``q`` and ``out`` must not overlap."""
-    dev, H = pages.device, q.shape[1]
-    batch.check(dev, q, out, lse)
-    qp = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)
-    op = _rows(out, dev, "out", H, layer.head_dim, torch.bfloat16)
-    if q.shape[0] != out.shape[0] or ws.device != dev:
+    dev, H = pages.index, q.shape[1] if q.dim() == 3 else 0
+    qp, qs, n = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)
+    op, os, m = _rows(out, dev, "out", H, layer.head_dim, torch.bfloat16)
+    batch.check(dev, n)
+    if n != m or ws.get_device() != dev:
         _bad("q and out must have the same rows, and the workspace the pages' device")
-    if lse is not None and (lse.dtype is not _F32 or lse.device != dev or not lse.is_contiguous() or
-                            lse.numel() < q.shape[0] * H):
-        _bad("lse must be a contiguous float32 tensor [rows, %d] on %s" % (H, dev))
-    if q.shape[0] == 0:
+    if lse is not None and (lse.dtype is not _F32 or lse.get_device() != dev or not lse.is_contiguous() or
+                            lse.numel() < n * H):
+        _bad("lse must be a contiguous float32 tensor [rows, %d] on GPU %s" % (H, dev))
+    if n == 0:
         return
     at = _Attention(H, 1 if causal else 0, float(softmax_scale), int(max_tokens))
-    _enqueue(lib().occam_cache_attend, dev, stream, pages.ref, layer.ref, batch.ref, ctypes.byref(at), *qp,
-             *op, None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    _enqueue(lib().occam_cache_attend, dev, stream, pages.ref, layer.ref, batch.ref, ctypes.byref(at), qp, qs,
+             op, os, None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes)

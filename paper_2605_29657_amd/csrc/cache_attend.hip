@@ -460,7 +460,7 @@ __device__ __forceinline__ void lds_barrier() {
 
 // A matrix phase reads its operands from LDS this many products ahead (the compiler by
 // itself reads two and waits for them).
-constexpr int kReads = 8;
+constexpr int kReads = 6;
 
 // The row blocks of a ragged batch, longest first: a workgroup that starts late on a long
 // one would end long after the others.  (In which order blocks of one length come is left
