@@ -177,6 +177,10 @@ __device__ __forceinline__ void note_cut(const AttendArgs& a, const Range& r, in
 // Few rows: 16 rows of one key head at a time, their keys dealt to the workgroup's four
 // waves in steps of 32, joined in LDS.  Bound by reading the codes once: a wave has the
 // loads of two steps in flight (8 KB each at d = 128) and several workgroups share a CU.
+// One row of each of 8 sequences of 16640 tokens, 32 key heads of 128: 175 us, 6.2 TB/s (a
+// large read reaches 5.7); of 64 sequences of 272 to 4608 tokens, 8 key heads: 55 us, 5.2
+// TB/s, about 8 us of it before the first codes arrive (rows, lengths, pages, codes: four
+// loads one after the other); of one sequence of 3011 tokens: 8 us, nothing but latency.
 // ---------------------------------------------------------------------------------------
 constexpr int kStep = 32, kFewWaves = 4, kFewRows = 16;
 constexpr int kFewUnit = kStep * kFewWaves;
@@ -438,9 +442,10 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
 //
 // What bounds it is the issue of vector instructions beside the matrix core: the products of
 // a tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about
-// as many.  A causal prompt of 4 x 3012 tokens, 32 heads of 128: 328 us, 906 TFLOP/s (a large
-// bf16 matrix product reaches 1342 here); text rows of 32 images, 16 to 512 of them over 272
-// to 4608 tokens: 248 us, 895 TFLOP/s.
+// as many.  A causal prompt of 4 x 3012 tokens, 32 heads of 128: 326 us, 912 TFLOP/s (a large
+// bf16 matrix product reaches 1342 here); 16 to 512 text rows of 32 images each, behind 256
+// to 4096 tokens, 32 heads on 8: 246 us, 901 TFLOP/s.  4 x 3000 tokens with 32 heads of 64:
+// 691 TFLOP/s, with 16 of 256: 749.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
@@ -459,12 +464,14 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // A matrix phase reads its operands from LDS this many products ahead (the compiler by
-// itself reads two and waits for them).
+// itself reads two and waits for them; with 8 and 12 the prompt takes 1 and 2 % longer).  It
+// runs at a higher wave priority than the vector phase beside it: 12 % at the prompt.
 constexpr int kReads = 6;
 
 // The row blocks of a ragged batch, longest first: a workgroup that starts late on a long
 // one would end long after the others.  (In which order blocks of one length come is left
-// open; it decides where they run, not what they give.)
+// open; it decides where they run, not what they give.)  5 us; the text rows below take
+// 264 us with it and 328 without.
 __global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entries, int blocks, int rows) {
     __shared__ int bin[kMaxOrder], sums[kMaxOrder / 64];
     const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
@@ -904,7 +911,8 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
 
 // Joins the parts of the row blocks that were cut: weights 2^(lse - max), each part's output
 // already divided by its own sum.  blockIdx.y: a place in the list of cut blocks; z: key
-// head; x: groups of 1024 / DP rows of the block, four elements a thread.
+// head; x: groups of 1024 / DP rows of the block, four elements a thread.  5 us, the latency
+// of a launch and three loads.
 template <int DP>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows) {
     constexpr int TE = DP / 4, NR = 256 / TE;
@@ -964,7 +972,9 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows)
 
 }  // namespace
 
-// Which form: more rows than two blocks of the few-row form go to the many-row form.
+// Which form: more rows than two blocks of the few-row form go to the many-row form (16 x 48
+// rows over 2048 tokens: 36 us few, 37 us many; 64 x 48 rows 112 and 96 us; 4 x 33 rows on
+// 32 key heads 68 and 57 us; 16 x 32 rows 29 us few, 36 us many).
 int attend_block_rows(const CacheView& c, const BatchView& b, int H) {
     const long long rows = (long long)b.max_rows * (H / c.Hkv);
     return rows <= 2 * kFewRows ? kFewRows : c.dp == 128 ? 256 : 128;
@@ -977,8 +987,10 @@ static long long attend_blocks(const CacheView& c, const BatchView& b, int H) {
 
 // Few rows: ranges per key head, the workgroups that are resident at once (registers: 4, 3
 // and 1 per CU at dp = 64, 128 and 256), no more than there is work at the longest.
-// Many rows: the most parts of a row block, enough for two workgroups per CU, of at least
-// kManyLeast tiles each.
+// Many rows: the most parts of a row block, as many as fill every CU once, of at least
+// kManyLeast tiles each.  (32 heads on 8 of 128: two prompts of 600 tokens take 24 us, 38 us
+// with parts for two workgroups per CU; 4 x 64 rows over 4096 tokens 38 and 54 us, with half
+// as many parts as CUs 43 us.)
 int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
     const long long blocks = b.n * attend_blocks(c, b, H);
     long long want, most;
@@ -986,7 +998,7 @@ int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_t
         want = 256 * (c.dp == 64 ? 4 : c.dp == 128 ? 3 : 1) / c.Hkv;
         most = blocks * ((max_tokens + kFewUnit - 1) / kFewUnit);
     } else {
-        want = 512 / (blocks * c.Hkv);
+        want = 256 / (blocks * c.Hkv);
         most = (max_tokens + kTile * kManyLeast - 1) / (kTile * kManyLeast);
     }
     want = want > most ? most : want;
@@ -1002,7 +1014,7 @@ int attend_streams(const CacheView& c, const BatchView& b, int H, long long max_
            2 * b.n * max_tokens * c.Hkv * c.dp > kLastLevelBytes;
 }
 
-// Whether a call sorts its row blocks: one more launch, where rows differ from sequence to
+// Whether a call sorts its row blocks: one more launch, so only where rows differ from sequence to
 // sequence and there are blocks for more than a round of the chip, up to a number whose
 // unevenness still shows at the end.
 int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges) {

@@ -8,16 +8,21 @@
 // the order in which threads run.  Freeing subtracts a reference; whoever takes the last
 // one clears the bit.  One workgroup plans a whole call (all or nothing needs one place that
 // knows the total); the per-sequence page lists are walked by a workgroup each.  What
-// bounds these kernels is latency: a handful of dependent loads and barriers.
+// bounds these kernels is latency: a handful of dependent loads and barriers.  Room for
+// one sequence's 131 tokens takes 5.1 us, for a token of 32 sequences 8.1 us, for 32 prompts (1300 pages of
+// 64) 11.7 us; forking 32 sequences 5.3 us, freeing them 4.2 us; what 64 pruned forks drop
+// 15.7 us, swapping their pages 4.1 us.
 #include "cache_internal.hpp"
 
 namespace occam {
 namespace {
 
-// Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences (fewer
-// waves at every barrier), 1024 beyond.  What a call reads again of its sequences is kept in
-// LDS for up to kNear of them, in the plan beyond; the pages it takes for up to kList of them.
-constexpr int kNear = 1024, kList = 4096;
+// Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences and, where
+// the host knows a bound, kSmallPages pages (fewer waves at every barrier), 1024 beyond: 1300
+// pages of 32 sequences take 11.7 us against 13.8, one page each 10.2 against 8.1.
+// What a call reads again of its sequences is kept in LDS for up to kNear of them, in the plan
+// beyond; the pages it takes for up to kList of them.
+constexpr int kSmallPages = 1024, kNear = 1024, kList = 4096;
 // Table entries of a fork call that one workgroup of 1024 threads copies by itself: 6.2 us
 // for 32 x 73 entries against 7.6 us in two launches, 7.7 against 8.0 us for 64 x 46.
 constexpr int kSmallTables = 4096;
@@ -465,7 +470,8 @@ static hipError_t plan_launch(hipStream_t s, A... args) {
 }
 
 hipError_t launch_pages_reserve(const PageView& p, const BatchView& b, int* plan, hipStream_t s) {
-    return b.n <= 256 ? plan_launch<256, pages_reserve<256>>(s, p, b, plan)
+    const bool small = b.n <= 256 && b.n * (((long long)b.max_rows >> p.shift) + 1) <= kSmallPages;
+    return small ? plan_launch<256, pages_reserve<256>>(s, p, b, plan)
                       : plan_launch<1024, pages_reserve<1024>>(s, p, b, plan);
 }
 
