@@ -102,6 +102,36 @@ __device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks
     const int entries = a.b.n * blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int total = 0, base = 0, mine = 0, before = 0;
     Block block = {};
+    Range r;
+    auto divide = [&]() {
+        r.each = (total + a.ranges - 1) / a.ranges;
+        r.each = r.each < least ? least : r.each;
+        // (Products past 2^31 would be past the end: ranges * each < total + ranges * least.)
+        r.start = w * r.each;
+        r.stop = r.start + r.each < total ? r.start + r.each : total;
+        r.entry = r.first = 0;
+    };
+    if (entries <= 64) {                   // every wave by itself
+        if (lane < entries) {
+            block = block_of(a, lane, blocks, rows);
+            mine = units_of(a, block, unit);
+        }
+        int s = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(s, o);
+            if (lane >= o) s += y;
+        }
+        total = __builtin_amdgcn_readlane(s, 63);
+        divide();
+        if (r.start >= total) return r;
+        const int from = __ffsll((unsigned long long)__ballot(r.start < s)) - 1;   // sums ascend
+        r.entry = from;
+        r.first = __builtin_amdgcn_readlane(s - mine, from);
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
+        r.block = Block{of(block.i), of(block.T), of(block.len), of(block.slot), of(block.r0), of(block.end)};
+        return r;
+    }
     // Exclusive prefix of the units of entries c .. c + NT - 1, and their sum.
     auto scan = [&](int c) {
         const int e = c + (int)threadIdx.x;
@@ -130,13 +160,7 @@ __device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks
         return sum;
     };
     for (int c = 0; c < entries; c += NT) total += scan(c);
-    Range r;
-    r.each = (total + a.ranges - 1) / a.ranges;
-    r.each = r.each < least ? least : r.each;
-    // (Products past 2^31 would be past the end: ranges * each < total + ranges * least.)
-    r.start = w * r.each;
-    r.stop = r.start + r.each < total ? r.start + r.each : total;
-    r.entry = r.first = 0;
+    divide();
     if (r.start >= total) return r;
     for (int c = 0; c < entries; c += NT) {
         const int sum = entries <= NT ? total : scan(c);
