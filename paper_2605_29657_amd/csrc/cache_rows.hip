@@ -263,9 +263,9 @@ struct Kept {
 // it once for HG heads of an item's keys or values and then has all their codes in flight;
 // they stay in registers between the search for the scale and the conversion (12 per unit).
 // A block takes `span` threads; workgroups with room for several take several head groups.
-// 64 forks' survivors, a tenth of 2880 tokens each, 8 heads of 128: 37 us for 38 MB of codes
+// 64 forks' survivors, a tenth of 2880 tokens each, 8 heads of 128: 36 us for 38 MB of codes
 // in and out, and the three neighbours in every group of four that a value's byte lies with:
-// 132 MB in all, 3.6 TB/s behind a chain of six loads.
+// 132 MB in all, 3.7 TB/s behind a chain of six loads.  (HG = 4 and 1: 3 us more, 8: 12.)
 template <int UPT, int HG>
 __global__ __launch_bounds__(kRowThreads) void cache_move(PageView p, CacheView c, int n,
                                                           const int* plan, const int* idx) {
@@ -447,7 +447,7 @@ hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const
     long long pages = (long long)n * p.max_pages;
     if (pages > p.num_pages) pages = p.num_pages;
     return with_units(p, c, [&](auto upt) {
-        constexpr int U = decltype(upt)::value, HG = U == 1 ? 4 : U == 2 ? 2 : 1;
+        constexpr int U = decltype(upt)::value, HG = U <= 2 ? 2 : 1;
         const dim3 grid(row_grid(p, c, pages * ((c.Hkv + HG - 1) / HG) * 2));
         return launch(cache_move<U, HG>, grid, dim3(kRowThreads), 0, s, p, c, n, plan, idx);
     });
