@@ -9,9 +9,9 @@
 // one clears the bit.  One workgroup plans a whole call (all or nothing needs one place that
 // knows the total); the per-sequence page lists are walked by a workgroup each.  What
 // bounds these kernels is latency: a handful of dependent loads and barriers.  Room for
-// one sequence's 131 tokens takes 5.1 us, for a token of 32 sequences 8.1 us, for 32 prompts (1300 pages of
-// 64) 11.7 us; forking 32 sequences 5.3 us, freeing them 4.2 us; what 64 pruned forks drop
-// 15.7 us, swapping their pages 4.1 us.
+// one sequence's 131 tokens takes 5.2 us, for a token of 32 sequences 6.6 us, for 32 prompts (1300 pages of
+// 64) 11.5 us; forking 32 sequences 5.3 us, freeing them 4.2 us; what 64 pruned forks drop
+// 13.5 us, swapping their pages 4.1 us.
 #include "cache_internal.hpp"
 
 namespace occam {
@@ -19,7 +19,7 @@ namespace {
 
 // Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences and, where
 // the host knows a bound, kSmallPages pages (fewer waves at every barrier), 1024 beyond: 1300
-// pages of 32 sequences take 11.7 us against 13.8, one page each 10.2 against 8.1.
+// pages of 32 sequences take 11.5 us against 13.8, one page each 9.6 against 6.6.
 // What a call reads again of its sequences is kept in LDS for up to kNear of them, in the plan
 // beyond; the pages it takes for up to kList of them.
 constexpr int kSmallPages = 1024, kNear = 1024, kList = 4096;
@@ -60,6 +60,8 @@ struct PlanShared {
     int bad;
     int near[4][kSeqs < kNear ? kSeqs : kNear];
     int list[kList];                       // pages taken, by rank
+    int rank[NT];                          // of a stretch of the map: ranks of the words' free
+    unsigned free[NT];                     // pages, and their bits
     int red[NT / 64];
 };
 
@@ -100,40 +102,63 @@ __device__ __forceinline__ unsigned first_word(const PageView& p) {
     return (int)threadIdx.x < (p.num_pages + 31) / 32 ? p.taken[threadIdx.x] : ~0u;
 }
 
+// The position of the set bit of f with k set bits below it.
+__device__ __forceinline__ int nth_bit(unsigned f, int k) {
+    int at = 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const int c = __popc(f & ((1u << o) - 1));
+        const bool up = k >= c;
+        k -= up ? c : 0;
+        at += up ? o : 0;
+        f = up ? f >> o : f;
+    }
+    return at;
+}
+
 // Takes the lowest `need` free pages, or none if there are not as many (false, in every
 // thread), and lists them by rank in list[0 .. need), which the caller may read after a barrier.
 template <int NT>
-__device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int need, int* red, int* list) {
+__device__ __forceinline__ bool take_free(const PageView& p, unsigned word0, int need, PlanShared<NT>& sh,
+                                          int* list) {
     if (need == 0) return true;
     const int words = (p.num_pages + 31) / 32;
-    int total, rank = block_scan<NT, int>(__popc(free_bits(p, threadIdx.x, word0)), &total, red);
+    int total, rank = block_scan<NT, int>(__popc(free_bits(p, threadIdx.x, word0)), &total, sh.red);
     const int total0 = total;
     int have = total0;
     for (int w0 = NT; w0 < words && have < need; w0 += NT) {
         const int w = w0 + threadIdx.x;
-        block_scan<NT, int>(__popc(free_bits(p, w, w < words ? p.taken[w] : ~0u)), &total, red);
+        block_scan<NT, int>(__popc(free_bits(p, w, w < words ? p.taken[w] : ~0u)), &total, sh.red);
         have += total;
     }
     if (have < need) return false;
-    // A word's owner only lists its pages by rank (the pages of a small call all come from
-    // one or two words, so one or two threads); placing them is every thread's work.
-    auto take = [&](int w, unsigned was, int r) {
-        unsigned f = free_bits(p, w, was), now = was;
-        for (; f && r < need; ++r) {
-            const int bit = __ffs(f) - 1;
-            f &= f - 1;
-            now |= 1u << bit;
-            list[r] = w * 32 + bit;
+    // A stretch of NT words, whose first free page has rank `base` and whose free pages are
+    // `count`: the words' owners mark what is taken, then any thread lists any page (those of
+    // a small call all come from one or two words).
+    auto take = [&](int w0, unsigned was, int base, int r, int count) {
+        const int w = w0 + threadIdx.x;
+        const unsigned f = free_bits(p, w, was);
+        if (f && base + r < need) {
+            const int n = need - base - r;       // free pages of this word that are taken
+            const unsigned below = n < __popc(f) ? (1u << nth_bit(f, n)) - 1 : ~0u;
+            p.taken[w] = was | (f & below);
         }
-        if (now != was) p.taken[w] = now;
+        sh.rank[threadIdx.x] = r;
+        sh.free[threadIdx.x] = f;
+        __syncthreads();
+        const int end = need - base < count ? need - base : count;
+        for (int x = threadIdx.x; x < end; x += NT) {
+            const int o = owner_of(sh.rank, NT, x);
+            list[base + x] = (w0 + o) * 32 + nth_bit(sh.free[o], x - sh.rank[o]);
+        }
     };
-    take(threadIdx.x, word0, rank);
+    take(0, word0, 0, rank, total0);
     int base = total0;
     for (int w0 = NT; w0 < words && base < need; w0 += NT) {
         const int w = w0 + threadIdx.x;
         const unsigned was = w < words ? p.taken[w] : ~0u;
-        rank = base + block_scan<NT, int>(__popc(free_bits(p, w, was)), &total, red);
-        take(w, was, rank);
+        rank = block_scan<NT, int>(__popc(free_bits(p, w, was)), &total, sh.red);   // (its barriers end
+        take(w0, was, base, rank, total);                                           // the use of sh.rank)
         base += total;
     }
     return true;
@@ -210,7 +235,7 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
     __syncthreads();
     const bool listed = need <= kList;
     int* list = listed ? sh.list : plan_record(plan, n, p.max_pages, 0);
-    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list)) {
+    if (sh.bad || !take_free<NT>(p, word0, need, sh, list)) {
         if (threadIdx.x == 0) {
             atomicOr(p.status, sh.bad ? sh.bad : (int)OCCAM_PAGES_FULL);
             write_header(plan, kPlanReserve, n, 0);
@@ -321,35 +346,38 @@ __global__ __launch_bounds__(256) void pages_free(PageView p, const int* seq) {
 // The first of m ascending distinct indices that is not its own position (m if none): the
 // first token dropped.  Probes side by side: at first 0, 1, 3, 7, ... (a pruned span has its
 // first gap early), then seven a round.
-__device__ __forceinline__ int first_gap(const int* idx, int m) {
-    int lo = 0, hi = m;                        // idx[lo - 1] == lo - 1; idx[hi] != hi or hi == m
-    {
-        constexpr int K = 14;
-        int at[K], good = 0;
+struct Gap {
+    static constexpr int K = 14;
+    int at[K];
+    __device__ __forceinline__ void probe(const int* idx, int m) {
 #pragma unroll
         for (int k = 0; k < K; ++k) at[k] = (1 << k) - 1 < m ? idx[(1 << k) - 1] - ((1 << k) - 1) : 1;
+    }
+    __device__ __forceinline__ int find(const int* idx, int m) const {
+        int good = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) good += at[k] == 0 && good == k;
-        lo = good ? 1 << (good - 1) : 0;
+        int lo = good ? 1 << (good - 1) : 0, hi = m;     // idx[lo - 1] == lo - 1; idx[hi] != hi or hi == m
         if (good < K && (1 << good) - 1 < hi) hi = (1 << good) - 1;
-    }
-    while (hi - lo > 0) {
-        const int step = (hi - lo + 7) >> 3;
-        int at[7], good = 0;
+        while (hi - lo > 0) {
+            const int step = (hi - lo + 7) >> 3;
+            int d[7];
+            good = 0;
 #pragma unroll
-        for (int k = 0; k < 7; ++k) {
-            const int x = lo + (k + 1) * step - 1;
-            at[k] = x < hi ? idx[x] - x : 1;
+            for (int k = 0; k < 7; ++k) {
+                const int x = lo + (k + 1) * step - 1;
+                d[k] = x < hi ? idx[x] - x : 1;
+            }
+#pragma unroll
+            for (int k = 0; k < 7; ++k) good += d[k] == 0 && good == k;
+            const int from = lo + good * step;
+            const int to = good < 7 ? lo + (good + 1) * step - 1 : hi;
+            lo = from;
+            hi = to < hi ? to : hi;
         }
-#pragma unroll
-        for (int k = 0; k < 7; ++k) good += at[k] == 0 && good == k;
-        const int from = lo + good * step;
-        const int to = good < 7 ? lo + (good + 1) * step - 1 : hi;
-        lo = from;
-        hi = to < hi ? to : hi;
+        return lo;
     }
-    return lo;
-}
+};
 
 // Compaction, first part: what every sequence drops and which fresh pages it gets, written
 // into the plan's page lists from the first changed page on.
@@ -372,6 +400,8 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
     for (int i = threadIdx.x; i < n; i += NT) {
         const int s = seq[i], a = start[i], m = span[i], o = off[i], c = off[i + 1] - o;
         int bad = 0, len = 0, now = 0, f = 0;
+        Gap gap;
+        gap.probe(idx + o, c < m ? c : 0);             // beside the length
         if (bad_slot(p, sh.seen, s)) {
             bad = OCCAM_PAGES_BAD_SEQ;
         } else {
@@ -380,7 +410,7 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
                 bad = OCCAM_PAGES_BAD_SPAN;
             } else if (c < m) {
                 now = len - m + c;
-                f = (a + first_gap(idx + o, c)) >> p.shift;
+                f = (a + gap.find(idx + o, c)) >> p.shift;
             } else {
                 f = (len + G - 1) >> p.shift;            // nothing dropped
             }
@@ -398,7 +428,7 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
     __syncthreads();
     const bool listed = need <= kList;
     int* list = listed ? sh.list : plan_record(plan, n, p.max_pages, 0);
-    if (sh.bad || !take_free<NT>(p, word0, need, sh.red, list)) {
+    if (sh.bad || !take_free<NT>(p, word0, need, sh, list)) {
         for (int i = threadIdx.x; i < n; i += NT) {
             g_news[i] = olds[i];
             g_first[i] = (olds[i] + G - 1) >> p.shift;
@@ -410,17 +440,16 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         return;
     }
     __syncthreads();
-    for (int r = threadIdx.x; r < need; r += NT) {
-        const int i = owner_of(sh.need, n, r), page = list[r];
+    auto place = [&](int x, int i) {
+        const int page = list[x];
         p.refs[page] = 1;
-        plan_pages(plan, n, p.max_pages, i)[first[i] + r - sh.need[i]] = page;
-    }
-    if (!listed) __syncthreads();          // the list lies where the records go
-    for (int x = threadIdx.x; x < need; x += NT) {
-        const int i = owner_of(sh.need, n, x), j = first[i] + x - sh.need[i];
-        const int now = news[i] - (j << p.shift);
+        plan_pages(plan, n, p.max_pages, i)[first[i] + x - sh.need[i]] = page;
+        return page;
+    };
+    auto record = [&](int x, int i, int page) {
+        const int j = first[i] + x - sh.need[i], now = news[i] - (j << p.shift);
         int* r = plan_record(plan, n, p.max_pages, x);
-        r[RK_PAGE] = listed ? list[x] : plan_pages(plan, n, p.max_pages, i)[j];
+        r[RK_PAGE] = page;
         r[RK_POS] = j << p.shift;
         r[RK_END] = now < G ? now : G;
         r[RK_SEQ] = i;
@@ -428,6 +457,17 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         r[RK_SPAN] = span[i];
         r[RK_OFF] = off[i];
         r[RK_COUNT] = off[i + 1] - off[i];
+    };
+    for (int x = threadIdx.x; x < need; x += NT) {
+        const int i = owner_of(sh.need, n, x), page = place(x, i);
+        if (listed) record(x, i, page);
+    }
+    if (!listed) {                         // the list lies where the records go
+        __syncthreads();
+        for (int x = threadIdx.x; x < need; x += NT) {
+            const int i = owner_of(sh.need, n, x);
+            record(x, i, plan_pages(plan, n, p.max_pages, i)[first[i] + x - sh.need[i]]);
+        }
     }
     if (threadIdx.x == 0) write_header(plan, kPlanKeep, n, need);
 }

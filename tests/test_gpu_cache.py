@@ -440,6 +440,49 @@ def test_many_sequences_and_a_large_pool():
     assert np.array_equal(bits[:70000], (pages.refs.cpu().numpy() > 0).astype(np.uint8))
 
 
+@pytest.mark.parametrize("n", [8, 300])
+def test_pages_are_taken_lowest_first_across_a_large_map(n):
+    # More words of the map than a workgroup has threads, with holes; 300 slots: the wide one.
+    num, page = 60000, 16
+    pages = cache.Pages(num, page, n, 40000)
+    plan = cache.plan(pages, n)
+    free, held = list(range(num)), {}
+
+    def reserve(seqs, counts):
+        others = [s for s in range(n) if s not in seqs and s not in held][:0 if n == 8 else 290]
+        order, rows = seqs + others, [c * page for c in counts] + [0] * len(others)
+        cache.reserve(pages, cache.Batch(len(order), seq=i32(order), row_offsets=i32(prefix(rows)),
+                                         max_rows=max(rows)), plan)
+        for s, c in zip(seqs, counts):
+            held[s] = held.get(s, []) + free[:c]
+            del free[:c]
+
+    def drop(seqs):
+        cache.free(pages, i32(seqs))
+        for s in seqs:
+            free.extend(held.pop(s))
+        free.sort()
+
+    reserve([0, 1, 2], [31, 8000, 33])
+    reserve([3, 0, 4], [200, 1, 32700])            # over the first stretch's end, of either form
+    drop([1, 3])
+    reserve([1, 5], [40, 7000])
+    reserve([6], [5000])                           # the holes' rest, then behind everything
+    drop([2, 4])
+    reserve([3, 2], [3, 30000])
+    assert pages.status.item() == 0
+    table, length = pages.table.cpu().numpy(), pages.length.tolist()
+    for s in range(n):
+        want = held.get(s, [])
+        assert length[s] == len(want) * page and table[s, :len(want)].tolist() == want
+    refs = np.zeros(num, int)
+    for want in held.values():
+        refs[want] += 1
+    assert np.array_equal(pages.refs.cpu().numpy(), refs)
+    bits = np.unpackbits(pages.taken.cpu().numpy().view(np.uint8), bitorder="little")
+    assert np.array_equal(bits[:num], refs)
+
+
 # --------------------------------------------------------------------------- attention
 def attend(c, seqs, rows, H, causal=True, scale=0.0, max_tokens=0, want_lse=True, q=None):
     n = sum(rows)
