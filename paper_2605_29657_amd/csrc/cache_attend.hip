@@ -473,6 +473,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
+constexpr int kManyParts = 1024;           // parts of a call (their outputs: 128 KB each at dp = 128)
 constexpr float kManyLift = 6.f, kManySlack = 8.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -1011,22 +1012,34 @@ static long long attend_blocks(const CacheView& c, const BatchView& b, int H) {
 
 // Few rows: ranges per key head, the workgroups that are resident at once (registers: 4, 3
 // and 1 per CU at dp = 64, 128 and 256), no more than there is work at the longest.
-// Many rows: the most parts of a row block, as many as fill every CU once, of at least
-// kManyLeast tiles each.  (32 heads on 8 of 128: two prompts of 600 tokens take 24 us, 38 us
-// with parts for two workgroups per CU; 4 x 64 rows over 4096 tokens 38 and 54 us, with half
-// as many parts as CUs 43 us.)
+// Many rows: the most parts of a row block, of at least kManyLeast tiles each.  A launch takes
+// as many rounds as it has workgroups per CU, each as long as a part (at the longest), the time
+// of about 4 tiles before and behind it and, where blocks are cut, of 8 for the part's output
+// to be written and joined.  (32 heads on 8 of 128: two prompts of 600 tokens, 160 row blocks
+// of 10 tiles, 24 us whole, 38 us in three parts; 4 x 64 rows over 4096 tokens 38 us in 8
+// parts, 43 in 4, 54 in 16; 64 heads, 18 x 30 rows over 12812 tokens 278 us in 5, 299 whole;
+// 32 heads of 64, 18 x 30 rows over 8000 tokens 71 us in 3, 131 whole.)
 int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
     const long long blocks = b.n * attend_blocks(c, b, H);
-    long long want, most;
     if (attend_block_rows(c, b, H) == kFewRows) {
-        want = 256 * (c.dp == 64 ? 4 : c.dp == 128 ? 3 : 1) / c.Hkv;
-        most = blocks * ((max_tokens + kFewUnit - 1) / kFewUnit);
-    } else {
-        want = 256 / (blocks * c.Hkv);
-        most = (max_tokens + kTile * kManyLeast - 1) / (kTile * kManyLeast);
+        const long long want = 256 * (c.dp == 64 ? 4 : c.dp == 128 ? 3 : 1) / c.Hkv;
+        const long long most = blocks * ((max_tokens + kFewUnit - 1) / kFewUnit);
+        const long long ranges = want > most ? most : want;
+        return ranges < 1 ? 1 : (int)ranges;
     }
-    want = want > most ? most : want;
-    return want < 1 ? 1 : (int)want;
+    const long long tiles = (max_tokens + kTile - 1) / kTile;
+    long long best = 0;
+    int parts = 1;
+    for (int p = 1; p <= 256 && (p == 1 || blocks * c.Hkv * p <= kManyParts); ++p) {
+        if (p > 1 && tiles < (long long)p * kManyLeast) break;
+        const long long rounds = (blocks * c.Hkv * p + 255) / 256;
+        const long long cost = rounds * ((tiles + p - 1) / p + (p > 1 ? 12 : 4));
+        if (p == 1 || cost < best) {
+            best = cost;
+            parts = p;
+        }
+    }
+    return parts;
 }
 
 // Whether the few-row form reads the codes past the caches: where nothing reads them twice
