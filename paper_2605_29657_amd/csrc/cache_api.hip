@@ -130,9 +130,8 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
 
 // The largest power of two up to `most` that divides x.
 int pow2_in(long long x, int most) {
-    int v = 1;
-    while (v < most && x % (2 * v) == 0) v *= 2;
-    return v;
+    const long long low = x & -x;
+    return low && low < most ? (int)low : most;
 }
 
 }  // namespace
@@ -177,7 +176,6 @@ occam_status occam_rotate(const occam_rotary* rotary, int32_t rows, const int32_
     for (int p = 0; p < r.pairs; ++p)
         if (r.axis[p] >= r.axes) return OCCAM_ERR_INVALID_ARG;
     RotArgs a;
-    memset(&a, 0, sizeof a);
     const long long e = dtype == OCCAM_F32 ? 4 : 2;
     int vec = dtype == OCCAM_F32 ? 4 : 8;
     vec = pow2_in(r.head_dim, vec);

@@ -146,14 +146,17 @@ struct RotTensor {
     int heads, first;            // heads before this tensor's
     long long src_stride, dst_stride;   // bytes
 };
-struct RotArgs {
-    RotTensor t[OCCAM_MAX_ROW_TENSORS];
+template <int TENSORS, int PAIRS>
+struct RotArgsOf {
+    static constexpr int kTensors = TENSORS, kPairs = PAIRS;
     int n, heads;                // tensors, heads over all of them
     int rows, d, pairs, axes, adjacent, inverse;
     const int* pos;
-    unsigned long long turn[OCCAM_MAX_PAIRS];
-    unsigned char axis[OCCAM_MAX_PAIRS];
+    RotTensor t[TENSORS];
+    unsigned long long turn[PAIRS];
+    unsigned char axis[PAIRS];
 };
+typedef RotArgsOf<OCCAM_MAX_ROW_TENSORS, OCCAM_MAX_PAIRS> RotArgs;
 
 // One row block of one sequence: its place in the batch, rows, length, slot, first row, and
 // the keys that its rows see (0 or less: none).
