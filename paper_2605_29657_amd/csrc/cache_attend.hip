@@ -473,7 +473,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
-constexpr int kManyParts = 1024;           // parts of a call (their outputs: 128 KB each at dp = 128)
+constexpr int kManyRounds = 4;             // of parts (their outputs: 128 KB each at dp = 128)
 constexpr float kManyLift = 6.f, kManySlack = 8.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -1027,19 +1027,21 @@ int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_t
         const long long ranges = want > most ? most : want;
         return ranges < 1 ? 1 : (int)ranges;
     }
-    const long long tiles = (max_tokens + kTile - 1) / kTile;
-    long long best = 0;
-    int parts = 1;
-    for (int p = 1; p <= 256 && (p == 1 || blocks * c.Hkv * p <= kManyParts); ++p) {
-        if (p > 1 && tiles < (long long)p * kManyLeast) break;
-        const long long rounds = (blocks * c.Hkv * p + 255) / 256;
-        const long long cost = rounds * ((tiles + p - 1) / p + (p > 1 ? 12 : 4));
-        if (p == 1 || cost < best) {
+    const long long tiles = (max_tokens + kTile - 1) / kTile, tasks = blocks * c.Hkv;
+    long long parts = 1, best = (tasks + 255) / 256 * (tiles + 4);
+    for (int rounds = 1; rounds <= kManyRounds; ++rounds) {
+        long long p = rounds * 256 / tasks;                    // as many as so many rounds hold
+        p = p < tiles / kManyLeast ? p : tiles / kManyLeast;
+        if (p < 2) continue;
+        const long long each = (tiles + p - 1) / p;
+        p = (tiles + each - 1) / each;
+        const long long cost = (tasks * p + 255) / 256 * (each + 12);
+        if (cost < best) {
             best = cost;
             parts = p;
         }
     }
-    return parts;
+    return (int)parts;
 }
 
 // Whether the few-row form reads the codes past the caches: where nothing reads them twice
