@@ -285,7 +285,7 @@ template <int NT, bool COPY>
 __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* src, const int* dst,
                                                 int* plan) {
     __shared__ unsigned seen[OCCAM_MAX_SLOTS / 32];
-    __shared__ int bad;
+    __shared__ int bad, near[COPY ? kSmallTables : 1];
     int* lens = plan_array(plan, n, PL_LENS);
     begin_call<NT>(p, seen, &bad);
     for (int i = threadIdx.x; i < n; i += NT) {
@@ -294,6 +294,7 @@ __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* sr
         if (bad_slot(p, seen, t) || s < 0 || s >= p.num_seqs || p.length[t] != 0) bad = 1;
         else len = p.length[s];
         lens[i] = len;
+        if (COPY) near[i] = len;
     }
     __syncthreads();
     if (bad) {
@@ -303,14 +304,14 @@ __global__ __launch_bounds__(NT) void fork_plan(PageView p, int n, const int* sr
     if (threadIdx.x == 0) write_header(plan, kPlanFork, n, 0);
     if (!COPY || bad) return;
     for (int x = threadIdx.x; x < n * p.max_pages; x += NT) {
-        const int i = x / p.max_pages, j = x - i * p.max_pages, len = lens[i];
+        const int i = x / p.max_pages, j = x - i * p.max_pages, len = near[i];
         if (j >= (len + (1 << p.shift) - 1) >> p.shift) continue;
         const int page = p.table[(size_t)src[i] * p.max_pages + j];
         p.table[(size_t)dst[i] * p.max_pages + j] = page;
         atomicAdd(&p.refs[page], 1);
     }
     for (int i = threadIdx.x; i < n; i += NT)
-        if (lens[i] > 0) p.length[dst[i]] = lens[i];
+        if (near[i] > 0) p.length[dst[i]] = near[i];
 }
 
 __global__ __launch_bounds__(256) void fork_copy(PageView p, int n, const int* src, const int* dst,
@@ -337,10 +338,14 @@ __global__ __launch_bounds__(256) void pages_free(PageView p, const int* seq) {
         return;
     }
     if (threadIdx.x == 0) len = atomicExch(&p.length[s], 0);   // a slot listed again gets 0
+    const int* row = p.table + (size_t)s * p.max_pages;
+    int page = (int)threadIdx.x < p.max_pages ? row[threadIdx.x] : 0;      // beside the length
     __syncthreads();
     const int pages = (len + (1 << p.shift) - 1) >> p.shift;
-    const int* row = p.table + (size_t)s * p.max_pages;
-    for (int j = threadIdx.x; j < pages; j += 256) drop_ref(p, row[j]);
+    for (int j = threadIdx.x; j < pages; j += 256) {
+        if (j >= 256) page = row[j];
+        drop_ref(p, page);
+    }
 }
 
 // The first of m ascending distinct indices that is not its own position (m if none): the
