@@ -483,6 +483,23 @@ def test_pages_are_taken_lowest_first_across_a_large_map(n):
     assert np.array_equal(bits[:num], refs)
 
 
+def test_freeing_pages_that_lie_far_apart():
+    # A page per round and sequence: a sequence's pages lie in as many words of the map.
+    n, rounds, page = 50, 70, 16
+    pages = cache.Pages(n * rounds, page, 2 * n, rounds)
+    plan = cache.plan(pages, n)
+    for _ in range(rounds):
+        cache.reserve(pages, cache.Batch(n, rows=page), plan)
+    cache.fork(pages, i32([3, 7]), i32([n, n + 1]), plan)
+    gone = [0, 3, 8, 49, 21, 7]
+    cache.free(pages, i32(gone))
+    refs = np.ones((rounds, n), int)
+    refs[:, [s for s in gone if s not in (3, 7)]] = 0          # 3 and 7 live on in their forks
+    assert np.array_equal(pages.refs.cpu().numpy(), refs.reshape(-1)) and pages.status.item() == 0
+    bits = np.unpackbits(pages.taken.cpu().numpy().view(np.uint8), bitorder="little")
+    assert np.array_equal(bits[:n * rounds], refs.reshape(-1))
+
+
 # --------------------------------------------------------------------------- attention
 def attend(c, seqs, rows, H, causal=True, scale=0.0, max_tokens=0, want_lse=True, q=None):
     n = sum(rows)
