@@ -213,9 +213,9 @@ typedef struct {
     int32_t max_tokens;   /* upper bound of the sequences' lengths (0: max_pages * page_tokens) */
 } occam_attention;
 
-/* Bytes of device workspace occam_cache_attend may use (0 for invalid arguments).  It
- * needs no initialisation and holds nothing between calls; calls that may overlap (streams,
- * graphs) need a workspace each. */
+/* Bytes of device workspace that occam_cache_attend with the same arguments may use (0 for
+ * invalid ones).  It needs no initialisation and holds nothing between calls; calls that may
+ * overlap (streams, graphs) need a workspace each. */
 size_t occam_cache_workspace_size(const occam_pages *pages, const occam_cache *cache,
                                   const occam_batch *batch, const occam_attention *attention);
 

@@ -26,8 +26,8 @@ occam_status pages_from(const occam_pages* p, bool arrays, PageView* out) {
     for (int s = 4; s <= 8; ++s)
         if (p->page_tokens == 1 << s) shift = s;
     if (!shift) return OCCAM_ERR_INVALID_ARG;
-    // Token positions are 32-bit.
-    if (((long long)p->max_pages << shift) >= (1LL << 31)) return OCCAM_ERR_UNSUPPORTED;
+    // Token positions are 32-bit, with room to round them up to pages and tiles.
+    if (((long long)p->max_pages << shift) > (1LL << 31) - 4096) return OCCAM_ERR_UNSUPPORTED;
     if (arrays && (!given(p->table, 4) || !given(p->length, 4) || !given(p->refs, 4) ||
                    !given(p->taken, 4) || !given(p->status, 4)))
         return OCCAM_ERR_INVALID_ARG;

@@ -90,6 +90,8 @@ def test_page_arrays(L, name, ptr):
 
 def test_positions_stay_in_32_bits(L):
     assert L.occam_pages_reset(pages(max_pages=1 << 25), None) == UNSUPPORTED
+    assert L.occam_pages_plan_size(pages(max_pages=(1 << 25) - 1), 1) == 0     # no room to round up
+    assert L.occam_pages_plan_size(pages(max_pages=(1 << 25) - 64), 1) > 0
     assert L.occam_cache_storage_size(pages(num_pages=1 << 24), 64, 128) == 0
 
 
