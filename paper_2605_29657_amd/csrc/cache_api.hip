@@ -85,7 +85,6 @@ bool rows_ok(const void* x, long long stride, const CacheView& c, int dtype) {
 struct AttendPlan {
     AttendArgs a;
     size_t off_l, off_cuts, total;
-    int ordered;
 };
 
 occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView& b,
@@ -109,21 +108,15 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     // Units of at least 64 keys of all row blocks (of at least 16 rows), at the longest.
     if ((double)b.n * ((double)b.max_rows * a.g / 16 + 1) * ((double)cap / 64 + 1) >= 2147483648.0)
         return OCCAM_ERR_UNSUPPORTED;
-    a.ranges = attend_ranges(c, b, a.H, most);
-    a.stream = attend_streams(c, b, a.H, most);
-    long long slots, cuts;
-    attend_slots(c, b, a.H, a.ranges, &slots, &cuts);
-    if (cuts > 65535) return OCCAM_ERR_UNSUPPORTED;        // a launch's grid.y
-    a.slots = (int)slots;
-    a.num_cuts = (int)cuts;
-    if (slots > 0) {
-        const size_t rows = (size_t)c.Hkv * slots * attend_block_rows(c, b, a.H);
+    const AttendShape& x = a.shape = attend_shape(c, b, a.H, most);
+    if (x.cuts > 65535) return OCCAM_ERR_UNSUPPORTED;      // a launch's grid.y
+    if (x.slots > 0) {
+        const size_t rows = (size_t)c.Hkv * x.slots * x.block_rows;
         out->off_l = align_up(rows * c.dp * sizeof(float));
         out->off_cuts = align_up(out->off_l + rows * sizeof(float));
-        out->total = align_up(out->off_cuts + (size_t)cuts * sizeof(int4));
+        out->total = align_up(out->off_cuts + (size_t)x.cuts * sizeof(int4));
     }
-    out->ordered = attend_ordered(c, b, a.H, a.ranges);        // (then nothing is cut)
-    if (out->ordered) out->total = align_up(out->ordered * sizeof(AttendBlock));
+    if (x.ordered) out->total = align_up(x.ordered * sizeof(AttendBlock));     // (then nothing is cut)
     if (out->total < kAlign) out->total = kAlign;
     return OCCAM_OK;
 }
@@ -390,7 +383,7 @@ occam_status occam_cache_attend(const occam_pages* pages, const occam_cache* cac
     a.part_o = static_cast<float*>(workspace);
     a.part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + ap.off_l);
     a.cuts = reinterpret_cast<int4*>(static_cast<char*>(workspace) + ap.off_cuts);
-    a.order = ap.ordered ? static_cast<AttendBlock*>(workspace) : nullptr;
+    a.order = a.shape.ordered ? static_cast<AttendBlock*>(workspace) : nullptr;
     return hip_ok(launch_cache_attend(a, stream));
 }
 

@@ -64,11 +64,11 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // ---------------------------------------------------------------------------------------
 typedef AttendBlock Block;
 // Later row blocks of every sequence come first: under a causal mask they are the long ones.
-__device__ __forceinline__ Block block_of(const AttendArgs& a, int entry, int blocks, int rows) {
+__device__ __forceinline__ Block block_of(const AttendArgs& a, int entry, int rows) {
     Block t;
     const int rb = entry / a.b.n;
     t.i = entry - rb * a.b.n;
-    t.r0 = (blocks - 1 - rb) * rows;
+    t.r0 = (a.shape.blocks - 1 - rb) * rows;
     t.T = row_count(a.b, t.i);
     t.slot = slot_of(a.b, t.i);
     const bool known = t.slot >= 0 && t.slot < a.pg.num_seqs;
@@ -94,17 +94,17 @@ struct Range {
     int each;                      // units per range
     Block block;                   // that row block
 };
-// Range `w` of a.ranges over the row blocks of the batch; all NT threads call it.  `red`:
+// Range `w` of a.shape.ranges over the row blocks of the batch; all NT threads call it.  `red`:
 // NT / 64 + 8 ints of LDS.
 template <int NT>
-__device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks, int rows, int unit,
+__device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int rows, int unit,
                                           int least, int* red) {
-    const int entries = a.b.n * blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int entries = a.b.n * a.shape.blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int total = 0, base = 0, mine = 0, before = 0;
     Block block = {};
     Range r;
     auto divide = [&]() {
-        r.each = (total + a.ranges - 1) / a.ranges;
+        r.each = (total + a.shape.ranges - 1) / a.shape.ranges;
         r.each = r.each < least ? least : r.each;
         // (Products past 2^31 would be past the end: ranges * each < total + ranges * least.)
         r.start = w * r.each;
@@ -113,7 +113,7 @@ __device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks
     };
     if (entries <= 64) {                   // every wave by itself
         if (lane < entries) {
-            block = block_of(a, lane, blocks, rows);
+            block = block_of(a, lane, rows);
             mine = units_of(a, block, unit);
         }
         int s = mine;
@@ -137,7 +137,7 @@ __device__ __forceinline__ Range range_of(const AttendArgs& a, int w, int blocks
         const int e = c + (int)threadIdx.x;
         mine = 0;
         if (e < entries) {
-            block = block_of(a, e, blocks, rows);
+            block = block_of(a, e, rows);
             mine = units_of(a, block, unit);
         }
         int s = mine;
@@ -198,9 +198,9 @@ __device__ __forceinline__ void note_cut(const AttendArgs& a, const Range& r, in
 }
 
 // ---------------------------------------------------------------------------------------
-// Few rows: 16 rows of one key head at a time, their keys dealt to the workgroup's four
-// waves in steps of 32, joined in LDS.  Bound by reading the codes once: a wave has the
-// loads of two steps in flight (8 KB each at d = 128) and several workgroups share a CU.
+// Few rows: 16 rows of one key head at a time (or 32: NR = 2), their keys dealt to the
+// workgroup's four waves in steps of 32, joined in LDS.  Bound by reading the codes once: a wave
+// has the loads of two steps in flight (8 KB each at d = 128) and several workgroups share a CU.
 // One row of each of 8 sequences of 16640 tokens, 32 key heads of 128: 175 us, 6.2 TB/s (a
 // large read reaches 5.7); of 64 sequences of 272 to 4608 tokens, 8 key heads: 55 us, 5.2
 // TB/s, about 8 us of it before the first codes arrive (rows, lengths, pages, codes: four
@@ -208,6 +208,9 @@ __device__ __forceinline__ void note_cut(const AttendArgs& a, const Range& r, in
 // ---------------------------------------------------------------------------------------
 constexpr int kStep = 32, kFewWaves = 4, kFewRows = 16;
 constexpr int kFewUnit = kStep * kFewWaves;
+constexpr long long kFewBytes = 64ll << 20;   // of codes: from here on 17 to 32 rows are one block
+// Workgroups of a CU: what the registers of 16 * NR rows leave room for.
+constexpr int few_resident(int dp, int nr) { return dp == 64 ? (nr == 1 ? 4 : 3) : dp == 128 ? (nr == 1 ? 3 : 2) : 1; }
 
 // Page numbers and scales of the 64 16-token groups around a wave's position, one per lane.
 struct Window {
@@ -215,37 +218,42 @@ struct Window {
     float ks, vs;
 };
 
-template <int DP, bool STREAM>
-__global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) void attend_few(AttendArgs a) {
+template <int DP, int NR, bool STREAM>
+__global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_few(AttendArgs a) {
     constexpr int NC = DP / 64;            // 64-element chunks of a row
+    constexpr int ROWS = kFewRows * NR;
     __shared__ float jo[kFewWaves][kFewRows][64 + 4];
-    __shared__ float jm[kFewWaves][kFewRows], jl[kFewWaves][kFewRows];
+    __shared__ float jm[kFewWaves][ROWS], jl[kFewWaves][ROWS];
     __shared__ int red[kFewWaves + 8];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 15, g4 = lane >> 4;
     const int w = blockIdx.x / a.c.Hkv, h = blockIdx.x - w * a.c.Hkv;
-    const int blocks = (a.b.max_rows * a.g + kFewRows - 1) / kFewRows;
-    const Range range = range_of<64 * kFewWaves>(a, w, blocks, kFewRows, kFewUnit, 1, red);
-    if (a.slots > 0 && h == 0 && threadIdx.x == 0) note_cut(a, range, w, kFewUnit);
+    const Range range = range_of<64 * kFewWaves>(a, w, ROWS, kFewUnit, 1, red);
+    if (a.shape.slots > 0 && h == 0 && threadIdx.x == 0) note_cut(a, range, w, kFewUnit);
     int entry = range.entry, at_unit = range.start - range.first;
-    for (int now = range.start; now < range.stop && entry < a.b.n * blocks; ++entry, at_unit = 0) {
-    const Block block = entry == range.entry ? range.block : block_of(a, entry, blocks, kFewRows);
+    for (int now = range.start; now < range.stop && entry < a.b.n * a.shape.blocks; ++entry, at_unit = 0) {
+    const Block block = entry == range.entry ? range.block : block_of(a, entry, ROWS);
     const int units = units_of(a, block, kFewUnit);
     if (units == 0) continue;
     const int take = units - at_unit < range.stop - now ? units - at_unit : range.stop - now;
     const bool whole = take == units;
     now += take;
     const int i = block.i, T = block.T, len = block.len, r0 = block.r0;
-    const int row = r0 + n, t = row / a.g, hh = h * a.g + row - t * a.g;
-    const bool live = t < T;
-    const int last = live ? (a.causal ? len - T + t : len - 1) : -1;       // last key seen
     const int lo = at_unit * kFewUnit;
     const int hi = lo + take * kFewUnit < block.end ? lo + take * kFewUnit : block.end;
     const int* table = a.pg.table + (size_t)block.slot * a.pg.max_pages;
 
     // Queries: reduction slots as the keys' 16-byte loads number them.
-    bf16x8 q[NC][2];
-    {
+    bf16x8 q[NR][NC][2];
+    int last[NR];                          // last key that the lane's rows see
+    float m[NR], l[NR];
+#pragma unroll
+    for (int b = 0; b < NR; ++b) {
+        const int row = r0 + b * kFewRows + n, t = row / a.g, hh = h * a.g + row - t * a.g;
+        const bool live = t < T;
+        last[b] = live ? (a.causal ? len - T + t : len - 1) : -1;
+        m[b] = -INFINITY;
+        l[b] = 0.f;
         const long long qrow = (long long)row_begin(a.b, i) + t;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -255,11 +263,10 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
                 u32x4 x = {0, 0, 0, 0};
                 if (live && e < a.c.d)
                     x = *reinterpret_cast<const u32x4*>(a.q + qrow * a.q_stride + (long long)hh * a.c.d + e);
-                q[c][f] = __builtin_bit_cast(bf16x8, x);
+                q[b][c][f] = __builtin_bit_cast(bf16x8, x);
             }
     }
-    f32x4 acc[NC][4] = {};
-    float m = -INFINITY, l = 0.f;
+    f32x4 acc[NR][NC][4] = {};
     int ref = kMinExp;
 
     const int groups = hi > 0 ? (hi + 15) >> 4 : 0;                        // of 16 tokens
@@ -304,52 +311,56 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
         }
     };
     auto compute = [&](int pos, Codes& x) {
-        f32x4 s[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    codes_bf16(x.k[u][c][0], x.k[u][c][1], x.ks[u]), q[c][0], s[u], 0, 0, 0);
-                s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    codes_bf16(x.k[u][c][2], x.k[u][c][3], x.ks[u]), q[c][1], s[u], 0, 0, 0);
-            }
-        }
-        float top = m;
+        f32x4 s[NR][2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = pos + u * 16 + g4 * 4 + e;
-                s[u][e] = key <= last && key < hi ? s[u][e] * a.scale2 : -INFINITY;
-                top = fmaxf(top, s[u][e]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const bf16x8 k = codes_bf16(x.k[u][c][2 * f], x.k[u][c][2 * f + 1], x.ks[u]);
+#pragma unroll
+                    for (int b = 0; b < NR; ++b)
+                        s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][c][f], s[b][u], 0, 0, 0);
+                }
         // The largest value scale so far; a step whose scales are larger shrinks the sums.
         const int e0 = exp_of(x.vs[0]), e1 = exp_of(x.vs[1]), em = e0 > e1 ? e0 : e1;
         const int now = em > ref ? em : ref;
-        const float base = top == -INFINITY ? 0.f : top;
-        const float fade = __builtin_amdgcn_exp2f(m - base);             // 0 while m is -inf
-        const int dref = ref - now < -126 ? -126 : ref - now;
-        const float fo = fade * exp_scale(dref);
-        m = top;
+        const float shrink = exp_scale(ref - now < -126 ? -126 : ref - now);
         ref = now;
-        float sum = 0.f;
-        f16x8 p;
+        f16x8 p[NR];
+        float fo[NR];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float y[4];
+        for (int b = 0; b < NR; ++b) {
+            float top = m[b];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = __builtin_amdgcn_exp2f(s[u][e] - base + kLift);
-                sum += y[e];
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = pos + u * 16 + g4 * 4 + e;
+                    s[b][u][e] = key <= last[b] && key < hi ? s[b][u][e] * a.scale2 : -INFINITY;
+                    top = fmaxf(top, s[b][u][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -INFINITY ? 0.f : top;
+            const float fade = __builtin_amdgcn_exp2f(m[b] - base);      // 0 while m is -inf
+            fo[b] = fade * shrink;
+            m[b] = top;
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = __builtin_amdgcn_exp2f(s[b][u][e] - base + kLift);
+                    sum += y[e];
+                }
+                const f16x2 a0 = round_f16(y[0], y[1]), a1 = round_f16(y[2], y[3]);
+                p[b][u * 4] = a0[0]; p[b][u * 4 + 1] = a0[1]; p[b][u * 4 + 2] = a1[0]; p[b][u * 4 + 3] = a1[1];
             }
-            const f16x2 a0 = round_f16(y[0], y[1]), a1 = round_f16(y[2], y[3]);
-            p[u * 4] = a0[0]; p[u * 4 + 1] = a0[1]; p[u * 4 + 2] = a1[0]; p[u * 4 + 3] = a1[1];
+            l[b] = l[b] * fade + sum;
         }
-        l = l * fade + sum;
         const float v0 = exp_scale(e0 - now < -126 ? -126 : e0 - now);
         const float v1 = exp_scale(e1 - now < -126 ? -126 : e1 - now);
         // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
@@ -368,9 +379,12 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                acc[c][d] *= fo;
-                acc[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    codes_f16(x.v[0][c][d], v0, x.v[1][c][d], v1), p, acc[c][d], 0, 0, 0);
+                const f16x8 v = codes_f16(x.v[0][c][d], v0, x.v[1][c][d], v1);
+#pragma unroll
+                for (int b = 0; b < NR; ++b) {
+                    acc[b][c][d] *= fo[b];
+                    acc[b][c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[b], acc[b][c][d], 0, 0, 0);
+                }
             }
     };
     {
@@ -389,58 +403,67 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 64 ? 4 : DP == 128 ? 3 : 1) v
         }
     }
     // The row's sum over the lane groups (each added its own tokens), then the waves join.
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
     constexpr float kDrop = 0x1p-14f;                       // undoes kLift
     __syncthreads();                                        // read for the row block before
-    if (g4 == 0) { jm[wave][n] = m; jl[wave][n] = l * kDrop; }
-    __syncthreads();
-    // 16 threads per row, four elements each of every 64-element chunk.
-    const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
-    const int rr = r0 + r, rt = rr / a.g, rh = h * a.g + rr - rt * a.g;
-    float top = jm[0][r];
 #pragma unroll
-    for (int x = 1; x < kFewWaves; ++x) top = fmaxf(top, jm[x][r]);
-    float wgt[kFewWaves], sum = 0.f;
-#pragma unroll
-    for (int x = 0; x < kFewWaves; ++x) {
-        wgt[x] = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(jm[x][r] - top);
-        sum += wgt[x] * jl[x][r];
-    }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const float lse2 = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;   // base 2
-    const float unref = exp_scale(ref - (int)kLift);
-    const long long orow = (long long)row_begin(a.b, i) + rt;
-    const size_t at = ((size_t)h * a.slots + 2 * w + (lo > 0 ? 0 : 1)) * kFewRows + r;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        if (c) __syncthreads();
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) jo[wave][n][g4 * 16 + e * 4 + d] = acc[c][d][e] * unref;
-        __syncthreads();
-        const int e0 = c * 64 + part * 4;
-        if (rt >= T || e0 >= a.c.d) continue;
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < kFewWaves; ++x)
-            y += wgt[x] * *reinterpret_cast<const f32x4*>(&jo[x][r][part * 4]);
-        y *= inv;
-        if (whole) {
-            ushort4 o;
-            o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
-            o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
-            o.z = __builtin_bit_cast(unsigned short, (__bf16)y[2]);
-            o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
-            *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)rh * a.c.d + e0) = o;
-        } else {
-            *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = y;
+    for (int b = 0; b < NR; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+        if (g4 == 0) {
+            jm[wave][b * kFewRows + n] = m[b];
+            jl[wave][b * kFewRows + n] = l[b] * kDrop;
         }
     }
-    if (part == 0 && rt < T) {
-        if (whole) { if (a.lse) a.lse[orow * a.H + rh] = lse2 * kLn2; }
-        else a.part_l[at] = lse2;
+    __syncthreads();
+    const float unref = exp_scale(ref - (int)kLift);
+    // 16 threads per row, four elements each of every 64-element chunk.
+    const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
+#pragma unroll
+    for (int b = 0; b < NR; ++b) {
+        const int rb = b * kFewRows + r, rr = r0 + rb, rt = rr / a.g, rh = h * a.g + rr - rt * a.g;
+        float top = jm[0][rb];
+#pragma unroll
+        for (int x = 1; x < kFewWaves; ++x) top = fmaxf(top, jm[x][rb]);
+        float wgt[kFewWaves], sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < kFewWaves; ++x) {
+            wgt[x] = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(jm[x][rb] - top);
+            sum += wgt[x] * jl[x][rb];
+        }
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float lse2 = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;   // base 2
+        const long long orow = (long long)row_begin(a.b, i) + rt;
+        const size_t at = ((size_t)h * a.shape.slots + 2 * w + (lo > 0 ? 0 : 1)) * ROWS + rb;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            if (b || c) __syncthreads();
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) jo[wave][n][g4 * 16 + e * 4 + d] = acc[b][c][d][e] * unref;
+            __syncthreads();
+            const int e0 = c * 64 + part * 4;
+            if (rt >= T || e0 >= a.c.d) continue;
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < kFewWaves; ++x)
+                y += wgt[x] * *reinterpret_cast<const f32x4*>(&jo[x][r][part * 4]);
+            y *= inv;
+            if (whole) {
+                ushort4 o;
+                o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
+                o.y = __builtin_bit_cast(unsigned short, (__bf16)y[1]);
+                o.z = __builtin_bit_cast(unsigned short, (__bf16)y[2]);
+                o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
+                *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)rh * a.c.d + e0) = o;
+            } else {
+                *reinterpret_cast<f32x4*>(a.part_o + at * DP + e0) = y;
+            }
+        }
+        if (part == 0 && rt < T) {
+            if (whole) { if (a.lse) a.lse[orow * a.H + rh] = lse2 * kLn2; }
+            else a.part_l[at] = lse2;
+        }
     }
     }
 }
@@ -497,7 +520,7 @@ constexpr int kReads = 6;
 // one would end long after the others.  (In which order blocks of one length come is left
 // open; it decides where they run, not what they give.)  5 us; the text rows below take
 // 264 us with it and 328 without.
-__global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entries, int blocks, int rows) {
+__global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entries) {
     __shared__ int bin[kMaxOrder], sums[kMaxOrder / 64];
     const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
     bin[e] = 0;
@@ -505,7 +528,7 @@ __global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entr
     Block b = {};
     int to = 0, at = 0;
     if (e < entries) {
-        b = block_of(a, e, blocks, rows);
+        b = block_of(a, e, a.shape.block_rows);
         const int units = units_of(a, b, kTile);
         to = kMaxOrder - 1 - (units < kMaxOrder ? units : kMaxOrder - 1);
         at = atomicAdd(&bin[to], 1);
@@ -551,16 +574,15 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 31, half = lane >> 5;
     // A workgroup per part of a row block; every sequence's last row block first.
-    const int blocks = (a.b.max_rows * a.g + ROWS - 1) / ROWS;
     const int task = blockIdx.x / a.c.Hkv, h = blockIdx.x - task * a.c.Hkv;
-    const int entry = task / a.ranges, part = task - entry * a.ranges;
-    const Block block = a.order ? a.order[entry] : block_of(a, entry, blocks, ROWS);
+    const int entry = task / a.shape.ranges, part = task - entry * a.shape.ranges;
+    const Block block = a.order ? a.order[entry] : block_of(a, entry, ROWS);
     const int units = units_of(a, block, kTile);
-    int each = (units + a.ranges - 1) / a.ranges;              // tiles of a part
+    int each = (units + a.shape.ranges - 1) / a.shape.ranges;              // tiles of a part
     each = each < kManyLeast ? kManyLeast : each;
     const int parts = (units + each - 1) / each;
-    if (a.slots > 0 && h == 0 && part == 0 && threadIdx.x == 0)
-        a.cuts[entry] = int4{parts > 1 ? entry : -1, parts, entry * a.ranges, 1};
+    if (a.shape.slots > 0 && h == 0 && part == 0 && threadIdx.x == 0)
+        a.cuts[entry] = int4{parts > 1 ? entry : -1, parts, entry * a.shape.ranges, 1};
     if (part >= parts) return;
     const bool whole = parts == 1;
     const int i = block.i, T = block.T, len = block.len, r0 = block.r0;
@@ -890,7 +912,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) - kManyLift : -INFINITY;
     const float f = exp_scale(ref);
-    const size_t at = ((size_t)h * a.slots + task) * ROWS + wave * 32 + n;
+    const size_t at = ((size_t)h * a.shape.slots + task) * ROWS + wave * 32 + n;
     if (whole) {
         // Through LDS, a part of the buffers for each wave (no wave reads a tile any more): a
         // lane's four elements of a row would leave as pieces of 16 bytes.
@@ -939,20 +961,20 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
 // head; x: groups of 1024 / DP rows of the block, four elements a thread.  5 us, the latency
 // of a launch and three loads.
 template <int DP>
-__global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows) {
+__global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     constexpr int TE = DP / 4, NR = 256 / TE;
     const int h = blockIdx.z;
     const int4 cut = a.cuts[blockIdx.y];
     if (cut.x < 0) return;
-    const int blocks = (a.b.max_rows * a.g + block_rows - 1) / block_rows;
-    const Block b = block_of(a, cut.x, blocks, block_rows);
+    const int block_rows = a.shape.block_rows;
+    const Block b = block_of(a, cut.x, block_rows);
     const int te = threadIdx.x % TE, rr = blockIdx.x * NR + threadIdx.x / TE;
     const int i = b.i, row = b.r0 + rr, t = row / a.g, hh = h * a.g + row - t * a.g;
     if (t >= b.T || te * 4 >= a.c.d) return;
     const int parts = cut.y;
     auto at = [&](int p) {
         const int slot = cut.z + (p ? p * cut.w - (cut.w - 1) : 0);
-        return ((size_t)h * a.slots + slot) * block_rows + rr;
+        return ((size_t)h * a.shape.slots + slot) * block_rows + rr;
     };
     float top = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
@@ -997,37 +1019,35 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int block_rows)
 
 }  // namespace
 
-// Which form: more rows than two blocks of the few-row form go to the many-row form (16 x 48
-// rows over 2048 tokens: 36 us few, 37 us many; 64 x 48 rows 112 and 96 us; 4 x 33 rows on
-// 32 key heads 68 and 57 us; 16 x 32 rows 29 us few, 36 us many).
-int attend_block_rows(const CacheView& c, const BatchView& b, int H) {
-    const long long rows = (long long)b.max_rows * (H / c.Hkv);
-    return rows <= 2 * kFewRows ? kFewRows : c.dp == 128 ? 256 : 128;
+// Rows of a row block.  More than 32 go to the many-row form (16 x 48 rows over 2048 tokens:
+// 36 us few, 37 us many; 64 x 48 rows 112 and 96 us; 4 x 33 rows on 32 key heads 68 and 57 us;
+// 16 x 32 rows 29 us few, 36 us many).  17 to 32 are one block of the few-row form where that
+// saves reading codes that no cache holds close (64 x 32 rows over 4096 tokens of 8 heads, 537
+// MB: 97 us against 180 in two blocks; 16 x 32 over 2048, 67 MB: 27 and 29; 4 x 32 over 4096,
+// 34 MB: 25 and 23.5), not at dp = 256, whose registers hold 16.
+static int attend_block_rows(const CacheView& c, long long rows, double bytes) {
+    if (rows > 2 * kFewRows) return c.dp == 128 ? 256 : 128;
+    return rows > kFewRows && c.dp <= 128 && bytes >= kFewBytes ? 2 * kFewRows : kFewRows;
 }
 
-static long long attend_blocks(const CacheView& c, const BatchView& b, int H) {
-    const int br = attend_block_rows(c, b, H);
-    return ((long long)b.max_rows * (H / c.Hkv) + br - 1) / br;
+// Ranges per key head of the few-row form: the workgroups that are resident at once, no more
+// than there is work at the longest.
+static long long few_ranges(const CacheView& c, int block_rows, long long entries, long long max_tokens) {
+    const long long want = 256 * few_resident(c.dp, block_rows / kFewRows) / c.Hkv;
+    const long long most = entries * ((max_tokens + kFewUnit - 1) / kFewUnit);
+    const long long ranges = want > most ? most : want;
+    return ranges < 1 ? 1 : ranges;
 }
 
-// Few rows: ranges per key head, the workgroups that are resident at once (registers: 4, 3
-// and 1 per CU at dp = 64, 128 and 256), no more than there is work at the longest.
-// Many rows: the most parts of a row block, of at least kManyLeast tiles each.  A launch takes
-// as many rounds as it has workgroups per CU, each as long as a part (at the longest), the time
-// of about 4 tiles before and behind it and, where blocks are cut, of 8 for the part's output
-// to be written and joined.  (32 heads on 8 of 128: two prompts of 600 tokens, 160 row blocks
-// of 10 tiles, 24 us whole, 38 us in three parts; 4 x 64 rows over 4096 tokens 38 us in 8
-// parts, 43 in 4, 54 in 16; 64 heads, 18 x 30 rows over 12812 tokens 278 us in 5, 299 whole;
-// 32 heads of 64, 18 x 30 rows over 8000 tokens 71 us in 3, 131 whole.)
-int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
-    const long long blocks = b.n * attend_blocks(c, b, H);
-    if (attend_block_rows(c, b, H) == kFewRows) {
-        const long long want = 256 * (c.dp == 64 ? 4 : c.dp == 128 ? 3 : 1) / c.Hkv;
-        const long long most = blocks * ((max_tokens + kFewUnit - 1) / kFewUnit);
-        const long long ranges = want > most ? most : want;
-        return ranges < 1 ? 1 : (int)ranges;
-    }
-    const long long tiles = (max_tokens + kTile - 1) / kTile, tasks = blocks * c.Hkv;
+// The most parts of a row block of the many-row form, of at least kManyLeast tiles each.  A
+// launch takes as many rounds as it has workgroups per CU, each as long as a part (at the
+// longest), the time of about 4 tiles before and behind it and, where blocks are cut, of 8 for
+// the part's output to be written and joined.  (32 heads on 8 of 128: two prompts of 600 tokens,
+// 160 row blocks of 10 tiles, 24 us whole, 38 us in three parts; 4 x 64 rows over 4096 tokens 38
+// us in 8 parts, 43 in 4, 54 in 16; 64 heads, 18 x 30 rows over 12812 tokens 278 us in 5, 299
+// whole; 32 heads of 64, 18 x 30 rows over 8000 tokens 71 us in 3, 131 whole.)
+static long long many_parts(long long tasks, long long max_tokens) {
+    const long long tiles = (max_tokens + kTile - 1) / kTile;
     long long parts = 1, best = (tasks + 255) / 256 * (tiles + 4);
     for (int rounds = 1; rounds <= kManyRounds; ++rounds) {
         long long p = rounds * 256 / tasks;                    // as many as so many rounds hold
@@ -1041,50 +1061,51 @@ int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_t
             parts = p;
         }
     }
-    return (int)parts;
+    return parts;
 }
 
-// Whether the few-row form reads the codes past the caches: where nothing reads them twice
-// (one row block per sequence and key head) and they may be more than the last-level cache
-// holds.  64 x 4096 tokens of 8 heads take 96 us against 106, with two row blocks each 208
-// against 177 us; 4 x 2048 tokens 14.7 against 14.3 us.
-int attend_streams(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
-    return attend_block_rows(c, b, H) == kFewRows && attend_blocks(c, b, H) == 1 &&
-           2 * b.n * max_tokens * c.Hkv * c.dp > kLastLevelBytes;
-}
-
-// Whether a call sorts its row blocks: one more launch, so only where rows differ from sequence to
-// sequence and there are blocks for more than a round of the chip, up to a number whose
-// unevenness still shows at the end.
-int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges) {
-    const long long entries = b.n * attend_blocks(c, b, H);
-    return b.off && ranges == 1 && attend_block_rows(c, b, H) > kFewRows && entries > 1 && entries <= kMaxOrder
-               ? (int)entries : 0;
-}
-
-// Slots for parts per key head, and places in the list of cut blocks: none where nothing
-// can be cut.
-void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
-                  long long* cuts) {
-    const long long blocks = b.n * attend_blocks(c, b, H);
-    const bool few = attend_block_rows(c, b, H) == kFewRows;
-    *slots = ranges == 1 ? 0 : few ? 2 * ranges : blocks * ranges;
-    *cuts = ranges == 1 ? 0 : few ? ranges : blocks;
+AttendShape attend_shape(const CacheView& c, const BatchView& b, int H, long long max_tokens) {
+    AttendShape x = {};
+    const long long rows = (long long)b.max_rows * (H / c.Hkv);
+    const double bytes = 2.0 * b.n * max_tokens * c.Hkv * c.dp;            // of codes, at the longest
+    x.block_rows = attend_block_rows(c, rows, bytes);
+    x.blocks = (int)((rows + x.block_rows - 1) / x.block_rows);
+    const long long entries = (long long)b.n * x.blocks;
+    x.few = x.block_rows <= 2 * kFewRows;
+    x.ranges = (int)(x.few ? few_ranges(c, x.block_rows, entries, max_tokens)
+                           : many_parts(entries * c.Hkv, max_tokens));
+    // The few-row form reads the codes past the caches where nothing reads them twice (one row
+    // block per sequence and key head) and they may be more than the last-level cache holds.  64
+    // x 4096 tokens of 8 heads take 96 us against 106, with two row blocks each 208 against 177
+    // us; 4 x 2048 tokens 14.7 against 14.3 us.
+    x.stream = x.few && x.blocks == 1 && bytes > kLastLevelBytes;
+    // A call sorts its row blocks, with one more launch, only where rows differ from sequence to
+    // sequence and there are blocks for more than a round of the chip, up to a number whose
+    // unevenness still shows at the end.
+    if (!x.few && b.off && x.ranges == 1 && entries > 1 && entries <= kMaxOrder) x.ordered = (int)entries;
+    // Slots for parts per key head, and places in the list of cut blocks: none where nothing can
+    // be cut.
+    if (x.ranges > 1) {
+        x.slots = x.few ? 2 * x.ranges : entries * x.ranges;
+        x.cuts = x.few ? x.ranges : entries;
+    }
+    return x;
 }
 
 template <int DP>
 static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
-    const int br = attend_block_rows(a.c, a.b, a.H);
-    const bool few = br == kFewRows;
-    const long long tasks = few ? a.ranges : a.b.n * attend_blocks(a.c, a.b, a.H) * a.ranges;
+    const AttendShape& x = a.shape;
+    const long long tasks = x.few ? x.ranges : (long long)a.b.n * x.blocks * x.ranges;
     const dim3 grid((unsigned)(tasks * a.c.Hkv));
     hipError_t e;
-    if (few) {
-        e = launch(a.stream ? attend_few<DP, true> : attend_few<DP, false>, grid, dim3(64 * kFewWaves), 0, s, a);
+    if (x.few) {
+        auto kernel = x.stream ? attend_few<DP, 1, true> : attend_few<DP, 1, false>;
+        if constexpr (DP <= 128)
+            if (x.block_rows > kFewRows) kernel = x.stream ? attend_few<DP, 2, true> : attend_few<DP, 2, false>;
+        e = launch(kernel, grid, dim3(64 * kFewWaves), 0, s, a);
     } else {
         if (a.order) {
-            const int blocks = (int)attend_blocks(a.c, a.b, a.H);
-            e = launch(attend_order, dim3(1), dim3(kMaxOrder), 0, s, a, a.b.n * blocks, blocks, br);
+            e = launch(attend_order, dim3(1), dim3(kMaxOrder), 0, s, a, x.ordered);
             if (e != hipSuccess) return e;
         }
         static_assert(32 * many_waves<DP>() == (DP == 128 ? 256 : 128), "rows of a block");
@@ -1094,8 +1115,8 @@ static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
                            : allow_lds(reinterpret_cast<const void*>(attend_many<DP>), bytes, done);
         if (e == hipSuccess) e = launch(attend_many<DP>, grid, dim3(64 * many_waves<DP>()), bytes, s, a);
     }
-    if (e != hipSuccess || a.slots == 0) return e;
-    return launch(attend_join<DP>, dim3(br / (1024 / DP), a.num_cuts, a.c.Hkv), dim3(256), 0, s, a, br);
+    if (e != hipSuccess || x.slots == 0) return e;
+    return launch(attend_join<DP>, dim3(x.block_rows / (1024 / DP), (unsigned)x.cuts, a.c.Hkv), dim3(256), 0, s, a);
 }
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {

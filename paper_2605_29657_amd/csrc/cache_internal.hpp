@@ -165,22 +165,29 @@ struct AttendBlock {
 };
 constexpr int kMaxOrder = 1024;          // row blocks that a call sorts by length at most
 
+// The form that an attention takes.
+struct AttendShape {
+    int few, stream;             // the few-row form; whether it reads the codes past the caches
+    int block_rows, blocks;      // rows of a row block; row blocks per sequence and key head
+    int ranges;                  // few rows: ranges of work per key head; many: parts of a block
+    int ordered;                 // row blocks that are sorted first (0: they run as they come)
+    long long slots, cuts;       // slots for parts per key head; places in the list of cut blocks
+};
+
 struct AttendArgs {
     PageView pg;
     CacheView c;
     BatchView b;
+    AttendShape shape;
     int H, g;                    // query heads, query heads per key head
     int causal;
     float scale2;                // softmax scale * log2(e)
-    int ranges;                  // few rows: ranges of work per key head; many: parts of a block
-    int stream;                  // few rows: the codes are read past the caches
-    int slots, num_cuts;         // slots for parts per key head; places in the list of cut blocks
     const unsigned short* q;
     unsigned short* out;
     long long q_stride, out_stride;     // elements
     float* lse;
     float *part_o, *part_l;      // [Hkv][slots][block rows][dp], [Hkv][slots][block rows]
-    int4* cuts;                  // [num_cuts]
+    int4* cuts;                  // [cuts]
     AttendBlock* order;          // row blocks, longest first, or NULL: as block_of numbers them
 };
 
@@ -202,13 +209,6 @@ hipError_t launch_cache_read(const PageView& p, const CacheView& c, const BatchV
 hipError_t launch_cache_move(const PageView& p, const CacheView& c, int n, const int* plan,
                              const int* idx, hipStream_t s);
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
-// Rows of a row block, division of the work, row blocks that are sorted (0: as they come) and
-// what is kept of parts, for the form that a call takes.
-int attend_block_rows(const CacheView& c, const BatchView& b, int H);
-int attend_ranges(const CacheView& c, const BatchView& b, int H, long long max_tokens);
-int attend_streams(const CacheView& c, const BatchView& b, int H, long long max_tokens);
-int attend_ordered(const CacheView& c, const BatchView& b, int H, int ranges);
-void attend_slots(const CacheView& c, const BatchView& b, int H, int ranges, long long* slots,
-                  long long* cuts);
+AttendShape attend_shape(const CacheView& c, const BatchView& b, int H, long long max_tokens);
 
 }  // namespace occam

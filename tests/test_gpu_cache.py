@@ -615,6 +615,30 @@ def test_attend_whatever_the_workspace_held(fill):
             M.check_attention(M.f64(out[x]), M.f64(lse[x]), M.f64(q[x]), c.k[s].x, c.v[s].x, True)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page,H,Hkv,d,T", [(16, 8, 2, 64, 8), (16, 3, 3, 40, 32), (64, 32, 8, 128, 7),
+                                            (32, 9, 1, 96, 3), (64, 32, 1, 128, 1), (128, 4, 4, 80, 17)])
+def test_attend_17_to_32_rows_in_one_block(page, H, Hkv, d, T, causal):
+    # Tables as long as those of a cache that the codes make worth it, most of them unused.
+    c = Cache(5, page, Hkv, d, num_pages=300, max_pages=1 << 21 - page.bit_length(), seed=page + T)
+    lens = [1, 700, 33, 0, 2600 if page > 16 else 900]
+    c.append([0, 1, 2, 4], [lens[x] for x in (0, 1, 2, 4)])
+    attend(c, [0, 1, 2, 3, 4], [T] * 5, H, causal)
+    attend(c, [4, 1, 0], [T, max(T - 1, 1), 1], H, causal)
+    # (A bound under which the caches hold the codes.)
+    some = (128 << 20) // (2 * 3 * Hkv * (64 if d <= 64 else 128))
+    attend(c, [4, 3, 2], [T, 0, T], H, causal, want_lse=False, max_tokens=some)
+    c.check()
+
+
+def test_attend_17_to_32_rows_of_unequal_scale():
+    for sizes in ([1e-6, 1.0, 1e-3, 1e4], [1e4, 1e-6, 1.0, 1e-3]):
+        c = Cache(1, 16, 1, 64, max_pages=1 << 16)
+        for z in sizes:
+            c.append([0], [48], size=z, k=c.rows(48, 0.3))
+        attend(c, [0], [6], 4)
+
+
 @pytest.mark.parametrize("H", [2, 8])
 def test_attend_more_row_blocks_than_threads(H):
     n = 300
