@@ -484,8 +484,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 // room), so four buffers are enough: tile t + 2 takes the place of t - 2, whose values B read
 // last in step t - 1.  The codes of two further tiles are on their way from memory.
 // (A barrier behind every phase: 337 us for the prompt below, against 328.)
-// With four waves (dp = 64 and 256: other waves of a CU are other workgroups) a tile is stored
-// in the vector phase before its matrix phase, with a barrier behind each and two buffers.
+// With four waves (up to 128 rows, and dp = 64 and 256) the other waves of a CU are another
+// workgroup's, if it has room for one, and a tile is stored in the vector phase before its
+// matrix phase, with a barrier behind each and two buffers.
 //
 // What bounds it is the issue of vector instructions beside the matrix core: the products of
 // a tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about
@@ -550,18 +551,16 @@ __global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entr
     if (e < entries) a.order[bin[to] + at] = b;
 }
 
-template <int DP> constexpr int many_waves() { return DP == 128 ? 8 : 4; }
-template <int DP> constexpr int many_bufs() { return many_waves<DP>() / 2; }
 // A buffer: keys [64] of 2 DP + 16 bytes, so that 16 rows' reads of 16 bytes fall on all
 // banks; values [tile of 32][16 tokens][half][DP][8 tokens], the 8 reduction slots of a lane.
 template <int DP> constexpr int many_keys() { return kTile * (DP * 2 + 16); }
 template <int DP> constexpr int many_buf() { return many_keys<DP>() + kTile * DP * 2; }
-template <int DP> constexpr int many_lds() { return many_bufs<DP>() * many_buf<DP>(); }
+template <int DP, int WAVES> constexpr int many_lds() { return WAVES / 2 * many_buf<DP>(); }
 
-template <int DP>
-__global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
-    constexpr int WAVES = many_waves<DP>(), THREADS = 64 * WAVES, ROWS = 32 * WAVES;
-    constexpr int AHEAD = WAVES / 4, BUFS = many_bufs<DP>();
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(AttendArgs a) {
+    constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+    constexpr int AHEAD = WAVES / 4, BUFS = WAVES / 2;
     constexpr int SETS = WAVES / 4;          // tiles in flight from memory
     constexpr int NK = DP / 16;              // 16-element steps of the score product
     constexpr int ND = DP / 32;              // 32-element tiles of the output
@@ -917,7 +916,7 @@ __global__ __launch_bounds__(64 * many_waves<DP>(), DP == 256 ? 1 : 2) void atte
         // Through LDS, a part of the buffers for each wave (no wave reads a tile any more): a
         // lane's four elements of a row would leave as pieces of 16 bytes.
         constexpr int PITCH = DP * 2 + 16, RPI = 64 / CH;          // rows per instruction
-        static_assert(WAVES * 32 * PITCH <= many_lds<DP>(), "output tile");
+        static_assert(WAVES * 32 * PITCH <= many_lds<DP, WAVES>(), "output tile");
         unsigned char* o = lds + wave * 32 * PITCH;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -1020,13 +1019,14 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 }  // namespace
 
 // Rows of a row block.  More than 32 go to the many-row form (16 x 48 rows over 2048 tokens:
-// 36 us few, 37 us many; 64 x 48 rows 112 and 96 us; 4 x 33 rows on 32 key heads 68 and 57 us;
-// 16 x 32 rows 29 us few, 36 us many).  17 to 32 are one block of the few-row form where that
+// 36 us few, 31 us many; 64 x 48 rows 112 and 68 us; 4 x 33 rows on 32 key heads 68 and 45 us;
+// 16 x 32 rows 29 us few, 36 us many), up to 128 with four waves, of which a CU holds two at dp =
+// 128 (64 x 48 rows: 96 us with eight, a third of them with rows).  17 to 32 are one block of the few-row form where that
 // saves reading codes that no cache holds close (64 x 32 rows over 4096 tokens of 8 heads, 537
 // MB: 97 us against 180 in two blocks; 16 x 32 over 2048, 67 MB: 27 and 29; 4 x 32 over 4096,
 // 34 MB: 25 and 23.5), not at dp = 256, whose registers hold 16.
 static int attend_block_rows(const CacheView& c, long long rows, double bytes) {
-    if (rows > 2 * kFewRows) return c.dp == 128 ? 256 : 128;
+    if (rows > 2 * kFewRows) return c.dp == 128 && rows > 128 ? 256 : 128;
     return rows > kFewRows && c.dp <= 128 && bytes >= kFewBytes ? 2 * kFewRows : kFewRows;
 }
 
@@ -1039,23 +1039,27 @@ static long long few_ranges(const CacheView& c, int block_rows, long long entrie
     return ranges < 1 ? 1 : ranges;
 }
 
+// Workgroups of a CU: what registers and LDS leave room for.
+static int many_resident(int dp, int block_rows) { return dp <= 128 && block_rows == 128 ? 2 : 1; }
+
 // The most parts of a row block of the many-row form, of at least kManyLeast tiles each.  A
-// launch takes as many rounds as it has workgroups per CU, each as long as a part (at the
-// longest), the time of about 4 tiles before and behind it and, where blocks are cut, of 8 for
-// the part's output to be written and joined.  (32 heads on 8 of 128: two prompts of 600 tokens,
-// 160 row blocks of 10 tiles, 24 us whole, 38 us in three parts; 4 x 64 rows over 4096 tokens 38
-// us in 8 parts, 43 in 4, 54 in 16; 64 heads, 18 x 30 rows over 12812 tokens 278 us in 5, 299
-// whole; 32 heads of 64, 18 x 30 rows over 8000 tokens 71 us in 3, 131 whole.)
-static long long many_parts(long long tasks, long long max_tokens) {
-    const long long tiles = (max_tokens + kTile - 1) / kTile;
-    long long parts = 1, best = (tasks + 255) / 256 * (tiles + 4);
-    for (int rounds = 1; rounds <= kManyRounds; ++rounds) {
-        long long p = rounds * 256 / tasks;                    // as many as so many rounds hold
+// launch takes as many rounds as it has workgroups beyond those resident, each as long as a part
+// (at the longest), the time of about 4 tiles before and behind it and, where blocks are cut, of
+// 8 for the part's output to be written, and of one for every part to be joined.  (32 heads on 8
+// of 128: two prompts of 600 tokens, 160 row blocks of 10 tiles, 24 us whole, 38 us in three
+// parts; 4 x 128 rows over 4096 tokens 29 us in 8 parts, 32 in 16; 32 x 64 rows over 4096 80 us
+// in two, 98 whole; 64 heads, 18 x 30 rows over 12812 tokens 278 us in 5, 299 whole; 32 heads of
+// 64, 18 x 30 rows over 8000 tokens 71 us in 3, 131 whole.)
+static long long many_parts(long long tasks, long long max_tokens, int resident) {
+    const long long tiles = (max_tokens + kTile - 1) / kTile, wgs = 256 * resident;
+    long long parts = 1, best = (tasks + wgs - 1) / wgs * (tiles + 4);
+    for (int half = 1; half <= 2 * kManyRounds; ++half) {
+        long long p = half * wgs / (2 * tasks);                // as many as so many half rounds hold
         p = p < tiles / kManyLeast ? p : tiles / kManyLeast;
         if (p < 2) continue;
         const long long each = (tiles + p - 1) / p;
         p = (tiles + each - 1) / each;
-        const long long cost = (tasks * p + 255) / 256 * (each + 12);
+        const long long cost = (tasks * p + wgs - 1) / wgs * (each + 12) + p;
         if (cost < best) {
             best = cost;
             parts = p;
@@ -1073,7 +1077,7 @@ AttendShape attend_shape(const CacheView& c, const BatchView& b, int H, long lon
     const long long entries = (long long)b.n * x.blocks;
     x.few = x.block_rows <= 2 * kFewRows;
     x.ranges = (int)(x.few ? few_ranges(c, x.block_rows, entries, max_tokens)
-                           : many_parts(entries * c.Hkv, max_tokens));
+                           : many_parts(entries * c.Hkv, max_tokens, many_resident(c.dp, x.block_rows)));
     // The few-row form reads the codes past the caches where nothing reads them twice (one row
     // block per sequence and key head) and they may be more than the last-level cache holds.  64
     // x 4096 tokens of 8 heads take 96 us against 106, with two row blocks each 208 against 177
@@ -1092,6 +1096,15 @@ AttendShape attend_shape(const CacheView& c, const BatchView& b, int H, long lon
     return x;
 }
 
+template <int DP, int WAVES>
+static hipError_t many_launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
+    constexpr int bytes = many_lds<DP, WAVES>();
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = bytes <= 65536
+        ? hipSuccess : allow_lds(reinterpret_cast<const void*>(attend_many<DP, WAVES>), bytes, done);
+    return e != hipSuccess ? e : launch(attend_many<DP, WAVES>, grid, dim3(64 * WAVES), bytes, s, a);
+}
+
 template <int DP>
 static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
     const AttendShape& x = a.shape;
@@ -1108,12 +1121,7 @@ static hipError_t attend_dp(const AttendArgs& a, hipStream_t s) {
             e = launch(attend_order, dim3(1), dim3(kMaxOrder), 0, s, a, x.ordered);
             if (e != hipSuccess) return e;
         }
-        static_assert(32 * many_waves<DP>() == (DP == 128 ? 256 : 128), "rows of a block");
-        constexpr int bytes = many_lds<DP>();
-        static std::atomic<uint64_t> done{0};
-        e = bytes <= 65536 ? hipSuccess
-                           : allow_lds(reinterpret_cast<const void*>(attend_many<DP>), bytes, done);
-        if (e == hipSuccess) e = launch(attend_many<DP>, grid, dim3(64 * many_waves<DP>()), bytes, s, a);
+        e = x.block_rows == 128 ? many_launch<DP, 4>(a, grid, s) : many_launch<128, 8>(a, grid, s);
     }
     if (e != hipSuccess || x.slots == 0) return e;
     return launch(attend_join<DP>, dim3(x.block_rows / (1024 / DP), (unsigned)x.cuts, a.c.Hkv), dim3(256), 0, s, a);
