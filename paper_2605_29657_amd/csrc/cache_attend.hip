@@ -488,12 +488,13 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 // workgroup's, if it has room for one, and a tile is stored in the vector phase before its
 // matrix phase, with a barrier behind each and two buffers.
 //
-// What bounds it is the issue of vector instructions beside the matrix core: the products of
-// a tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about
-// as many.  A causal prompt of 4 x 3012 tokens, 32 heads of 128: 326 us, 912 TFLOP/s (a large
-// bf16 matrix product reaches 1342 here); 16 to 512 text rows of 32 images each, behind 256
-// to 4096 tokens, 32 heads on 8: 246 us, 901 TFLOP/s.  4 x 3000 tokens with 32 heads of 64:
-// 691 TFLOP/s, with 16 of 256: 749.
+// What bounds it is the issue of vector instructions beside the matrix core (the products of a
+// tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about as
+// many) and the card's power: the prompt below takes 274 us on constant data, at a higher clock,
+// as a large library product gains 28 % there.  A causal prompt of 4 x 3012 tokens, 32 heads of
+// 128: 326 us, 912 TFLOP/s (large library products 1342 to 1415); 16 to 512 text rows of 32
+// images each, behind 256 to 4096 tokens, 32 heads on 8: 246 us, 901 TFLOP/s.  4 x 3000 tokens
+// with 32 heads of 64: 691 TFLOP/s, with 16 of 256: 749.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
