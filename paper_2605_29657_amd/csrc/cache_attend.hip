@@ -210,7 +210,9 @@ constexpr int kStep = 32, kFewWaves = 4, kFewRows = 16;
 constexpr int kFewUnit = kStep * kFewWaves;
 constexpr long long kFewBytes = 64ll << 20;   // of codes: from here on 17 to 32 rows are one block
 // Workgroups of a CU: what the registers of 16 * NR rows leave room for.
-constexpr int few_resident(int dp, int nr) { return dp == 64 ? (nr == 1 ? 4 : 3) : dp == 128 ? (nr == 1 ? 3 : 2) : 1; }
+constexpr int few_resident(int dp, int nr) {
+    return dp == 64 ? (nr == 1 ? 4 : 3) : dp == 128 ? (nr == 1 ? 3 : 2) : 1;
+}
 
 // Page numbers and scales of the 64 16-token groups around a wave's position, one per lane.
 struct Window {
