@@ -1021,14 +1021,15 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 
 }  // namespace
 
-// Rows of a row block.  More than 32 go to the many-row form (16 x 48 rows over 2048 tokens:
-// 36 us few, 31 us many; 64 x 48 rows 112 and 68 us; 4 x 33 rows on 32 key heads 68 and 45 us;
-// 16 x 32 rows 29 us few, 36 us many), up to 128 with four waves, of which a CU holds two
-// workgroups at dp = 128 (64 x 48 rows: 96 us with eight waves, a third of them with rows; a prompt
-// of 4 x 3012 tokens: 370 us with four, 341 with eight beside it).  17 to 32 are one block of the few-row form where that
-// saves reading codes that no cache holds close (64 x 32 rows over 4096 tokens of 8 heads, 537
-// MB: 97 us against 180 in two blocks; 16 x 32 over 2048, 67 MB: 27 and 29; 4 x 32 over 4096,
-// 34 MB: 25 and 23.5), not at dp = 256, whose registers hold 16.
+// Rows of a row block.  More than 32 go to the many-row form (16 x 48 rows over 2048 tokens: 36
+// us few, 31 us many; 64 x 48 rows 112 and 68 us; 4 x 33 rows on 32 key heads 68 and 45 us; 16 x
+// 32 rows 29 us few, 36 us many), up to 128 with four waves, of which a CU holds two workgroups
+// at dp = 128 (64 x 48 rows: 96 us with eight waves, a third of them with rows; a prompt of 4 x
+// 3012 tokens: 370 us with four, 341 with eight beside it).
+// 17 to 32 are one block of the few-row form where that saves reading codes that no cache holds
+// close (64 x 32 rows over 4096 tokens of 8 heads, 537 MB: 97 us against 180 in two blocks; 16 x
+// 32 over 2048, 67 MB: 27 and 29; 4 x 32 over 4096, 34 MB: 25 and 23.5), not at dp = 256, whose
+// registers hold 16.
 static int attend_block_rows(const CacheView& c, long long rows, double bytes) {
     if (rows > 2 * kFewRows) return c.dp == 128 && rows > 128 ? 256 : 128;
     return rows > kFewRows && c.dp <= 128 && bytes >= kFewBytes ? 2 * kFewRows : kFewRows;
