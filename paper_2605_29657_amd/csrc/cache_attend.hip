@@ -621,7 +621,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
         v.ks = 1.f;
         v.ve = kMinExp;                      // no group: no claim on the reference
         const size_t at = (size_t)v.page * a.c.Hkv + h;
-        size_t off = at * a.c.block;         // past the end: page 0, whose codes are masked
+        size_t off = at * a.c.block;         // past the part's end: page 0, whose codes are masked
         if (base + lane < groups) {
             v.ks = a.c.ks[at];
             v.ve = exp_of(a.c.vs[at]);
@@ -672,13 +672,14 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
         vto[u] = HALF + unit * 32;
     }
     auto mask_tile = [&](int pos, Raw& r) {
-        // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
-        if (pos + kTile > len) {
+        // Codes behind the part's last key may be anything, NaN among it (behind the sequence's
+        // end, and page 0's in place of groups that no row sees): 0 * NaN is not 0.
+        if (pos + kTile > hi) {
 #pragma unroll
             for (int u = 0; u < UV; ++u)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const int left = len - (pos + group_of(u) * 16 + (hf + 2 * k) * 4);
+                    const int left = hi - (pos + group_of(u) * 16 + (hf + 2 * k) * 4);
                     const unsigned keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
                     r.v[u][k][0] &= keep;
                     r.v[u][k][1] &= keep;
