@@ -224,8 +224,11 @@ size_t occam_cache_workspace_size(const occam_pages *pages, const occam_cache *c
  * out: bfloat16 [rows][H][d], rows q_row_stride / out_row_stride elements apart (multiples
  * of 8, 16-byte aligned).  row_lse (nullable): float32 [rows][H], the natural-log softmax
  * normaliser over those keys, in the layout of occam_score's row_lse.  A row that sees no
- * key gets zeros and -infinity.  q and out must not overlap.  max_tokens only sizes the launch and the workspace; a
- * longer sequence is still attended to in full. */
+ * key gets zeros and -infinity.  Probabilities are rounded to float16 (2^-11 of them), sums are
+ * float32; a key whose weight (its probability times its block's scale) is far below the row's
+ * largest one adds its share to within 2^-26 of that weight.  q and out must not overlap.
+ * max_tokens only sizes the launch and the workspace; a longer sequence is still attended to in
+ * full. */
 occam_status occam_cache_attend(const occam_pages *pages, const occam_cache *cache,
                                 const occam_batch *batch, const occam_attention *attention,
                                 const void *q, int64_t q_row_stride, void *out,

@@ -13,12 +13,12 @@
 // load gives four elements of a group of four tokens.
 //
 // 8 bits to matrix operands: one conversion instruction turns two codes and a power-of-two
-// scale into two bf16 (keys) or f16 (values) numbers.  Keys are exact in bf16.  Values are
-// converted relative to the largest value scale met so far (`ref`), which keeps them within
-// f16's range; they are exact down to 2^-15 of it, and off by at most 2^-25 below.
-// Probabilities are rounded to f16 (11 bits, half a step 2^-12: a bf16 probability, 2^-9,
-// would cost as much accuracy as rounding the output) times 2^14, so that they lose nothing
-// before 2^-28.  Maxima, sums and outputs are float32.
+// scale into two bf16 (keys) or f16 (values) numbers.  Keys are exact in bf16, and so are
+// values in f16, converted relative to the largest value scale met so far (`ref`) as long as
+// all scales met lie within 2^kSpread (see Scales below).  Probabilities are rounded to f16
+// (half a step, 2^-11 of them; a bf16 one, 2^-8, would cost as much as rounding the output
+// does), held times 2^14 (few rows) or 2^9 (many): they keep all bits down to 2^-28 and
+// 2^-23, and are off by at most 2^-39 and 2^-34 below.  Maxima, sums and outputs are float32.
 #include <type_traits>
 
 #include "cache_internal.hpp"
@@ -55,6 +55,24 @@ __device__ __forceinline__ f16x2 round_f16(float a, float b) {     // to nearest
     return f16x2{(_Float16)a, (_Float16)b};
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// ---------------------------------------------------------------------------------------
+// Scales.  Pages have scales of their own, 2^-100 to 2^120.  A row's output is a sum of codes
+// times weights, w_j = p_j s_j, and a weight is held relative to ref.  While the scales met lie
+// within 2^kFewSpread or 2^kManySpread, the row's largest weight is at least 2^-spread of that,
+// so weights are within 2^-27 of the largest, and the powers of two between scale and ref are
+// in the converted values.  From the first keys on that pass the spread (which may be keys that
+// some rows do not see, or give no probability) a row's sums are in units of an exponent of its
+// own, ceil(W - m), W = the largest of (score + scale's exponent, base 2) of the keys it has
+// seen, m its maximum; the exponent that gives a weight has the scale in it, and values are bare
+// codes.  So what a row does not see, or gives little, moves nothing in its output by more than
+// 2^-26 of its largest weight, and ordinary caches, whose scales differ by a few binades, never
+// get there.  (Keeping rows' own units in the common loop costs 25 %: its registers spill.
+// Watching the spread costs 0.3 us of 11 in a small call and 1.5 % of the prompt below.)
+// ---------------------------------------------------------------------------------------
+constexpr int kFewSpread = 12, kManySpread = 7;
+// The unit of a row's sums: the exponent of its largest weight (`w`) over its maximum.
+__device__ __forceinline__ int unit_of(float w, float m) { return w == -INFINITY ? 0 : (int)ceilf(w - m); }
 
 // ---------------------------------------------------------------------------------------
 // Division of work.  Per key head there is a row block of so many rows of every sequence,
@@ -226,6 +244,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
     constexpr int ROWS = kFewRows * NR;
     __shared__ float jo[kFewWaves][kFewRows][64 + 4];
     __shared__ float jm[kFewWaves][ROWS], jl[kFewWaves][ROWS];
+    __shared__ int ju[kFewWaves][ROWS];
     __shared__ int red[kFewWaves + 8];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int n = lane & 15, g4 = lane >> 4;
@@ -269,7 +288,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
             }
     }
     f32x4 acc[NR][NC][4] = {};
-    int ref = kMinExp;
+    int ref = kMinExp, least = kMaxExp;    // the largest and the least value scale so far
 
     const int groups = hi > 0 ? (hi + 15) >> 4 : 0;                        // of 16 tokens
     Window win;
@@ -312,7 +331,16 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
             x.vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(win.vs), src));
         }
     };
-    auto compute = [&](int pos, Codes& x) {
+    // Whether the scales met, this step's among them, lie within the spread.
+    auto regular = [&](const Codes& x) {
+        const int e0 = exp_of(x.vs[0]), e1 = exp_of(x.vs[1]), hi2 = e0 > e1 ? e0 : e1, lo2 = e0 < e1 ? e0 : e1;
+        return (hi2 > ref ? hi2 : ref) - (lo2 < least ? lo2 : least) <= kFewSpread;
+    };
+    // OWN: rows have units of their own (`unit`, and `most`, their largest weight's exponent).
+    int unit[NR];
+    float most[NR];
+    auto compute = [&](auto own, int pos, Codes& x) {
+        constexpr bool OWN = decltype(own)::value;
         f32x4 s[NR][2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -326,15 +354,19 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
                         s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][c][f], s[b][u], 0, 0, 0);
                 }
         // The largest value scale so far; a step whose scales are larger shrinks the sums.
-        const int e0 = exp_of(x.vs[0]), e1 = exp_of(x.vs[1]), em = e0 > e1 ? e0 : e1;
-        const int now = em > ref ? em : ref;
-        const float shrink = exp_scale(ref - now < -126 ? -126 : ref - now);
-        ref = now;
+        const int e0 = exp_of(x.vs[0]), e1 = exp_of(x.vs[1]);
+        float shrink = 1.f;
+        if constexpr (!OWN) {
+            const int em = e0 > e1 ? e0 : e1, el = e0 < e1 ? e0 : e1, now = em > ref ? em : ref;
+            shrink = exp_scale(ref - now < -126 ? -126 : ref - now);       // (-126: of sums of zero)
+            ref = now;
+            least = el < least ? el : least;
+        }
         f16x8 p[NR];
         float fo[NR];
 #pragma unroll
         for (int b = 0; b < NR; ++b) {
-            float top = m[b];
+            float top = m[b], weight = -INFINITY;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -342,12 +374,24 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
                     const int key = pos + u * 16 + g4 * 4 + e;
                     s[b][u][e] = key <= last[b] && key < hi ? s[b][u][e] * a.scale2 : -INFINITY;
                     top = fmaxf(top, s[b][u][e]);
+                    if constexpr (OWN) weight = fmaxf(weight, s[b][u][e] + (float)(u ? e1 : e0));
                 }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -INFINITY ? 0.f : top;
             const float fade = __builtin_amdgcn_exp2f(m[b] - base);      // 0 while m is -inf
             fo[b] = fade * shrink;
+            float by[2] = {0.f, 0.f};
+            if constexpr (OWN) {
+                weight = fmaxf(weight, __shfl_xor(weight, 16));
+                weight = fmaxf(weight, __shfl_xor(weight, 32));
+                most[b] = fmaxf(most[b], weight);
+                const int now = unit_of(most[b], base);
+                fo[b] = __builtin_amdgcn_exp2f(m[b] - base + (float)(unit[b] - now));
+                unit[b] = now;
+                by[0] = (float)(now - e0);
+                by[1] = (float)(now - e1);
+            }
             m[b] = top;
             float sum = 0.f;
 #pragma unroll
@@ -357,14 +401,14 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
                 for (int e = 0; e < 4; ++e) {
                     y[e] = __builtin_amdgcn_exp2f(s[b][u][e] - base + kLift);
                     sum += y[e];
+                    if constexpr (OWN) y[e] = __builtin_amdgcn_exp2f(s[b][u][e] - base + kLift - by[u]);
                 }
                 const f16x2 a0 = round_f16(y[0], y[1]), a1 = round_f16(y[2], y[3]);
                 p[b][u * 4] = a0[0]; p[b][u * 4 + 1] = a0[1]; p[b][u * 4 + 2] = a1[0]; p[b][u * 4 + 3] = a1[1];
             }
             l[b] = l[b] * fade + sum;
         }
-        const float v0 = exp_scale(e0 - now < -126 ? -126 : e0 - now);
-        const float v1 = exp_scale(e1 - now < -126 ? -126 : e1 - now);
+        const float v0 = OWN ? 1.f : exp_scale(e0 - ref), v1 = OWN ? 1.f : exp_scale(e1 - ref);
         // Codes behind the sequence's end may be anything, NaN among it: 0 * NaN is not 0.
         if (pos + kStep > len) {
 #pragma unroll
@@ -393,15 +437,28 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
         Codes x[2];
         const int stride = kStep * kFewWaves;
         int pos = lo + wave * kStep;
+        const std::false_type shared;
+        const std::true_type own;
         if (pos < hi) load_step(pos, x[0]);
         while (pos < hi) {
             if (pos + stride < hi) load_step(pos + stride, x[1]);
-            compute(pos, x[0]);
+            if (!regular(x[0])) break;
+            compute(shared, pos, x[0]);
             pos += stride;
             if (pos >= hi) break;
             if (pos + stride < hi) load_step(pos + stride, x[0]);
-            compute(pos, x[1]);
+            if (!regular(x[1])) break;
+            compute(shared, pos, x[1]);
             pos += stride;
+        }
+#pragma unroll
+        for (int b = 0; b < NR; ++b) {
+            unit[b] = ref;
+            most[b] = m[b] + (float)ref;
+        }
+        for (; pos < hi; pos += stride) {          // (one step at a time: these are rare)
+            load_step(pos, x[0]);
+            compute(own, pos, x[0]);
         }
     }
     // The row's sum over the lane groups (each added its own tokens), then the waves join.
@@ -414,10 +471,10 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
         if (g4 == 0) {
             jm[wave][b * kFewRows + n] = m[b];
             jl[wave][b * kFewRows + n] = l[b] * kDrop;
+            ju[wave][b * kFewRows + n] = unit[b];
         }
     }
     __syncthreads();
-    const float unref = exp_scale(ref - (int)kLift);
     // 16 threads per row, four elements each of every 64-element chunk.
     const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
 #pragma unroll
@@ -426,13 +483,19 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
         float top = jm[0][rb];
 #pragma unroll
         for (int x = 1; x < kFewWaves; ++x) top = fmaxf(top, jm[x][rb]);
-        float wgt[kFewWaves], sum = 0.f;
+        // A wave's outputs are in units of 2^(m + unit), and come together in the largest such;
+        // their mean is taken before the unit, as a sum of values could pass float32's range.
+        float wgt[kFewWaves], units = -INFINITY, sum = 0.f;
 #pragma unroll
         for (int x = 0; x < kFewWaves; ++x) {
-            wgt[x] = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(jm[x][rb] - top);
-            sum += wgt[x] * jl[x][rb];
+            wgt[x] = jm[x][rb] + (float)ju[x][rb];
+            units = fmaxf(units, wgt[x]);
+            sum += top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(jm[x][rb] - top) * jl[x][rb];
         }
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int x = 0; x < kFewWaves; ++x)
+            wgt[x] = sum > 0.f ? __builtin_amdgcn_exp2f(wgt[x] - units) : 0.f;
+        const float inv = sum > 0.f ? kDrop / sum : 0.f, up = sum > 0.f ? __builtin_amdgcn_exp2f(units - top) : 0.f;
         const float lse2 = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;   // base 2
         const long long orow = (long long)row_begin(a.b, i) + rt;
         const size_t at = ((size_t)h * a.shape.slots + 2 * w + (lo > 0 ? 0 : 1)) * ROWS + rb;
@@ -442,7 +505,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) jo[wave][n][g4 * 16 + e * 4 + d] = acc[b][c][d][e] * unref;
+                for (int e = 0; e < 4; ++e) jo[wave][n][g4 * 16 + e * 4 + d] = acc[b][c][d][e];
             __syncthreads();
             const int e0 = c * 64 + part * 4;
             if (rt >= T || e0 >= a.c.d) continue;
@@ -450,7 +513,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 #pragma unroll
             for (int x = 0; x < kFewWaves; ++x)
                 y += wgt[x] * *reinterpret_cast<const f32x4*>(&jo[x][r][part * 4]);
-            y *= inv;
+            y = y * inv * up;
             if (whole) {
                 ushort4 o;
                 o.x = __builtin_bit_cast(unsigned short, (__bf16)y[0]);
@@ -475,7 +538,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 // tile of 64 keys and values through LDS.  The tile is converted to 16 bits once, on its way
 // into LDS (a wave that converted its own operands would spend as long on that as on the
 // products).  The running maximum only moves the sums when some row's maximum passed the
-// one in use by more than 2^8: probabilities are held times 2^6, so they stay below 2^14.
+// one in use by more than 2^6: probabilities are held times 2^9, so they stay within 2^15.
 //
 // A wave alternates between a vector phase (the softmax of tile t) and a matrix phase (the
 // output of tile t, the scores of t + 1).  With eight waves, the two of a SIMD belong to two
@@ -501,7 +564,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
 constexpr int kManyRounds = 4;             // of parts (their outputs: 128 KB each at dp = 128)
-constexpr float kManyLift = 6.f, kManySlack = 8.f;
+constexpr float kManyLift = 9.f, kManySlack = 6.f;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ float max_over_halves(float x) {            // lanes l and l ^ 32
@@ -607,11 +670,12 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
     bf16x8 q[NK];
     f32x16 acc[ND] = {};
     float m = -INFINITY, l = 0.f;            // m: the maximum in use, in base 2
-    int ref = kMinExp;                       // of the values summed; the same in every wave
+    int ref = kMinExp, unit = kMinExp;       // of the values summed (the same in every wave), and
+                                             // at last the exponent that the sums are in units of
 
     const int groups = hi > 0 ? (hi + 15) >> 4 : 0;
     // 64 groups of 16 tokens, one per lane, and the next 64: where a group's codes lie, its
-    // scales, and the largest value exponent of the four groups of its tile.
+    // scales, and the largest and the least value exponent of the groups of its tile, packed.
     struct Win { int page; unsigned lo, hi; float ks; int ve, top; } win, nxt;
     auto win_page = [&](int base) {
         const int x = base + lane;
@@ -620,19 +684,25 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
     auto win_scales = [&](int base, Win& v) {
         v.ks = 1.f;
         v.ve = kMinExp;                      // no group: no claim on the reference
+        int least = kMaxExp;
         const size_t at = (size_t)v.page * a.c.Hkv + h;
         size_t off = at * a.c.block;         // past the part's end: page 0, whose codes are masked
         if (base + lane < groups) {
             v.ks = a.c.ks[at];
-            v.ve = exp_of(a.c.vs[at]);
+            v.ve = least = exp_of(a.c.vs[at]);
             off += (size_t)(((base + lane) << 4) & ((1 << a.pg.shift) - 1)) * DP;
         }
         v.lo = (unsigned)off;
         v.hi = (unsigned)(off >> 32);
         int o = __builtin_amdgcn_mov_dpp(v.ve, 0xB1, 15, 15, true);      // lane ^ 1
-        v.top = v.ve > o ? v.ve : o;
-        o = __builtin_amdgcn_mov_dpp(v.top, 0x4E, 15, 15, true);         // lane ^ 2
-        v.top = v.top > o ? v.top : o;
+        int top = v.ve > o ? v.ve : o;
+        o = __builtin_amdgcn_mov_dpp(top, 0x4E, 15, 15, true);           // lane ^ 2
+        top = top > o ? top : o;
+        o = __builtin_amdgcn_mov_dpp(least, 0xB1, 15, 15, true);
+        least = least < o ? least : o;
+        o = __builtin_amdgcn_mov_dpp(least, 0x4E, 15, 15, true);
+        least = least < o ? least : o;
+        v.top = top * 512 + (least - kMinExp);
     };
     // A tile on its way from memory to LDS: codes, and what converts them.  Unit x of a
     // group of 16 tokens: 16 codes of a key row; two elements of 8 tokens' values.
@@ -692,7 +762,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
         if (x < 2) {
             *reinterpret_cast<bf16x8*>(d + kto[u] + x * 16) = codes_bf16(r.k[u][x * 2], r.k[u][x * 2 + 1], r.sk[u]);
         } else {
-            const float sc = exp_scale(r.sv[u] - to < -126 ? -126 : r.sv[u] - to);
+            const float sc = exp_scale(r.sv[u] - to < -126 ? -126 : r.sv[u] - to);     // (-126: no group)
             *reinterpret_cast<f16x8*>(d + vto[u] + (x - 2) * 16) =
                 codes_f16(r.v[u][0][x - 2], sc, r.v[u][1][x - 2], sc);
         }
@@ -782,6 +852,45 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
             }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
+    // The softmax behind scales past the spread, e the four groups' exponents.
+    auto own_softmax = [&](int pos, const int* e, float& most) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float x = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int u = g >> 1, at = (g & 1) * 8 + i;
+                const int key = pos + g * 16 + (i >> 2) * 8 + half * 4 + (i & 3);
+                s[u][at] = key <= last && key < hi ? s[u][at] : -INFINITY;
+                x = fmaxf(x, s[u][at]);
+            }
+            x = max_over_halves(x) * a.scale2;
+            top = fmaxf(top, x);
+            most = fmaxf(most, x + (float)e[g]);
+        }
+        const float now = fmaxf(m, top), from = now == -INFINITY ? 0.f : now;
+        const int to = unit_of(most, from);
+        const float fo = __builtin_amdgcn_exp2f(m - from + (float)(unit - to));      // 0 while m is -inf
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= fo;
+        l *= __builtin_amdgcn_exp2f(m - from);
+        m = now;
+        unit = to;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = s[g >> 1][(g & 1) * 8 + i];
+                sum[(g >> 1) * 2 + (i & 1)] += __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale2, kManyLift - from));
+                p[g][i] = (_Float16)__builtin_amdgcn_exp2f(
+                    __builtin_fmaf(x, a.scale2, kManyLift - from - (float)(to - e[g])));
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
     if (hi > lo) {
         const int tiles = (hi - lo + kTile - 1) / kTile;
         int base = lo >> 4;                      // windows count from the part's first group
@@ -800,8 +909,15 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
             if (in == 32) win_scales(base + 64, nxt);
         };
         auto fetch = [&](int tile, Raw& r) { load_tile(tile, win, r); };
-        int refs[3];                             // of the tiles from the present one on
-        int to = kMinExp;
+        // The references of the tiles from the present one on: the largest value scale up to there
+        // (`to`: of the tile being stored).  `stop`: the first tile whose scales pass the spread.
+        int refs[3], to = kMinExp, least = kMaxExp, stop = tiles;
+        auto refer = [&](int x, int packed) {
+            const int top = packed >> 9, low = (packed & 511) + kMinExp;
+            to = top > to ? top : to;
+            least = low < least ? low : least;
+            stop = to - least > kManySpread && x < stop ? x : stop;
+        };
         Raw start[AHEAD];
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) fetch(x, start[x]);
@@ -825,7 +941,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) {
             mask_tile(lo + x * kTile, start[x]);
-            to = start[x].top > to ? start[x].top : to;
+            refer(x, start[x].top);
             store_tile(start[x], x % BUFS, to);
             refs[x] = to;
         }
@@ -848,11 +964,11 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
         if constexpr (AHEAD == 1) {
             matrix(scores, 0, 0, nothing);
             lds_barrier();
-            for (int tile = 0; tile < tiles; ++tile) {
+            for (int tile = 0; tile < stop; ++tile) {
                 const int pos = lo + tile * kTile;
                 if (pos < wave_hi) softmax(pos, refs[0]);
                 mask_tile(pos + kTile, raw[0]);
-                to = raw[0].top > to ? raw[0].top : to;
+                refer(tile + 1, raw[0].top);
                 store_tile(raw[0], (tile + 1) % BUFS, to);
                 window(tile + 1 + SETS);
                 fetch(tile + 1 + SETS, raw[0]);
@@ -869,7 +985,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
             auto coming = [&](int x, Raw& r) {
                 mask_tile(lo + x * kTile, r);
                 window(x + SETS);
-                to = r.top > to ? r.top : to;
+                refer(x, r.top);
             };
             auto beside = [&](int i, int x, Raw& r) {
                 if (i % 2 == 0 && i < 8) store_part(r, x % BUFS, to, 0, i / 2);
@@ -904,17 +1020,50 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
                 refs[2] = to;
                 if (!behind) lds_barrier();
             };
-            for (int tile = 0; tile < tiles; tile += SETS) {
+            // (`stop` is known a tile ahead at least, and the same in every wave.)
+            for (int tile = 0; tile < stop; tile += SETS) {
                 step(tile, raw[0]);
-                if (tile + 1 < tiles) step(tile + 1, raw[SETS - 1]);
+                if (tile + 1 < stop) step(tile + 1, raw[SETS - 1]);
             }
             lds_barrier();                       // the last tile has been read by everyone
+        }
+        unit = ref;
+        if (stop < tiles) {
+            // Scales past the spread: a tile at a time, bare codes and rows' own units.
+            float most = m + (float)ref;             // the rows' largest weights' exponents
+            for (int tile = stop; tile < tiles; ++tile) {
+                const int pos = lo + tile * kTile, base = pos >> 4;
+                Win v;
+                v.page = win_page(base);
+                win_scales(base, v);
+                Raw& r = raw[0];
+                load_tile(0, v, r);
+                mask_tile(pos, r);
+#pragma unroll
+                for (int u = 0; u < UK; ++u) r.sv[u] = 0;
+                store_tile(r, 0, 0);
+                lds_barrier();
+                if (pos < wave_hi) {
+                    int e[4];
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) e[g] = __builtin_amdgcn_readlane(v.ve, g);
+                    matrix(scores, 0, 0, nothing);
+                    own_softmax(pos, e, most);
+                    const unsigned char* vd = lds + HALF + (half * DP + n) * 16;
+#pragma unroll
+                    for (int i = 0; i < OUT; ++i)
+                        acc[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            *reinterpret_cast<const f16x8*>(vd + (i / ND) * 2 * DP * 16 + (i % ND) * 512), p[i / ND],
+                            acc[i % ND], 0, 0, 0);
+                }
+                lds_barrier();
+            }
         }
     }
     l += __shfl_xor(l, 32);
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __builtin_amdgcn_logf(l) - kManyLift : -INFINITY;
-    const float f = exp_scale(ref);
+    const float f = exp_scale(unit);
     const size_t at = ((size_t)h * a.shape.slots + task) * ROWS + wave * 32 + n;
     if (whole) {
         // Through LDS, a part of the buffers for each wave (no wave reads a tile any more): a
@@ -960,9 +1109,12 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
 }
 
 // Joins the parts of the row blocks that were cut: weights 2^(lse - max), each part's output
-// already divided by its own sum.  blockIdx.y: a place in the list of cut blocks; z: key
+// already divided by its own sum.  (They are multiplied in halves, and held times 2^-12: a part of
+// little weight can hold values 2^220 times the others', and a sum of values could pass
+// float32's range.)  blockIdx.y: a place in the list of cut blocks; z: key
 // head; x: groups of 1024 / DP rows of the block, four elements a thread.  5 us, the latency
 // of a launch and three loads.
+constexpr float kJoinDrop = 12.f;
 template <int DP>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     constexpr int TE = DP / 4, NR = 256 / TE;
@@ -997,14 +1149,14 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) most = fmaxf(most, l[u]);
         if (most == -INFINITY) continue;
-        const float fade = __builtin_amdgcn_exp2f(top - most);
-        sum *= fade;
-        y *= fade;
+        const float fade = __builtin_amdgcn_exp2f(0.5f * (top - most));
+        sum *= fade * fade;
+        y = y * fade * fade;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float wgt = __builtin_amdgcn_exp2f(l[u] - most);
-            sum += wgt;
-            y += wgt * o[u];
+            const float root = __builtin_amdgcn_exp2f(0.5f * (l[u] - most) - kJoinDrop / 2);
+            sum += root * root;
+            y += o[u] * root * root;
         }
         top = most;
     }
@@ -1017,7 +1169,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     o.w = __builtin_bit_cast(unsigned short, (__bf16)y[3]);
     *reinterpret_cast<ushort4*>(a.out + orow * a.out_stride + (long long)hh * a.c.d + te * 4) = o;
     if (te == 0 && a.lse)
-        a.lse[orow * a.H + hh] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        a.lse[orow * a.H + hh] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum) + kJoinDrop) * kLn2 : -INFINITY;
 }
 
 }  // namespace
