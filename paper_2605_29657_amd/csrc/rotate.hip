@@ -4,8 +4,9 @@
 // The angle.  A position's turns are kept as a 64-bit fraction, F_p = inv_freq_p / 2 pi in
 // units of 2^-64, so position * F_p modulo 2^64 is the angle's fraction of a turn with no
 // rounding but F's own: exact where a float32 product (error 2^-24 of the angle) would
-// be wrong by a radian at position 10^7.  Sine and cosine take the fraction in
-// half-turns, rounded once to float32 (an angle error of pi 2^-25).
+// be wrong by a radian at position 10^7.  Sine and cosine are taken of its 24 leading bits,
+// which float32 holds, and turned by what is left, r: s + c r and c - s r (|r| is below 2^-22,
+// and r^2 / 2 below 2^-45).
 //
 // Bound by memory: every element is read and written once, and a row's sines and cosines
 // are computed once for all heads of all tensors (queries and keys share a launch), staged
@@ -61,12 +62,14 @@ __global__ __launch_bounds__(kRotThreads) void rotate(Args a, int rows_per) {
     for (int i = threadIdx.x; i < rows * a.pairs; i += kRotThreads) {
         const int r = i / a.pairs, p = i - r * a.pairs;
         const int pos = a.pos[(size_t)(row0 + r) * a.axes + a.axis[p]];
-        const long long turn = (long long)((unsigned long long)(long long)pos * a.turn[p]);
-        // Signed fraction of a turn in 2^-32, then half-turns in (-1, 1].
-        const float half = (float)(int)((turn + (1ll << 31)) >> 32) * 0x1p-31f;
+        const unsigned long long turn = (unsigned long long)(long long)pos * a.turn[p];
+        // To the nearest 2^-24 of a turn, signed, in half-turns; the rest in radians.
+        const long long lead = (long long)(turn + (1ull << 39)) >> 40;
+        const float left = (float)(int)((long long)(turn - ((unsigned long long)lead << 40)) >> 8) * 0x1.921fb6p-54f;
         float s, c;
-        sincospif(half, &s, &c);
-        cs[i] = make_float2(c, a.inverse ? -s : s);
+        sincospif((float)(int)lead * 0x1p-23f, &s, &c);
+        const float s1 = __builtin_fmaf(c, left, s), c1 = __builtin_fmaf(-s, left, c);
+        cs[i] = make_float2(c1, a.inverse ? -s1 : s1);
     }
     __syncthreads();
     typedef Pack<T, N> V;
