@@ -172,7 +172,7 @@ occam_status occam_pages_free(const occam_pages *pages, int32_t n, const int32_t
  * stay whose index within the span is listed in kept_idx[kept_offsets[i] ..
  * kept_offsets[i + 1]), ascending -- the lists of occam_select / occam_prune (what a list
  * that is not ascending leaves is undefined, but comes from the same sequence).  Tokens
- * outside the span stay.  The pages from the first dropped token's on are replaced by fresh
+ * outside the span stay.  kept_idx is not NULL, also where every list is empty.  The pages from the first dropped token's on are replaced by fresh
  * ones, so pages shared with other sequences are not touched; the fresh pages must be free
  * while the old ones are still held.  Every layer's occam_cache_move has to be enqueued
  * with the same plan, kept_idx and kept_offsets before any later call that takes pages. */

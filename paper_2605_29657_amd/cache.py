@@ -323,6 +323,13 @@ def free(pages, seq, stream=None):
     _enqueue(lib().occam_pages_free, dev, stream, pages.ref, seq.numel(), _ints(seq, dev, "seq"))
 
 
+def _lists(kept_idx, kept_offsets, dev):
+    """Pointers of the survivors' lists.  A list of no survivors may have no address: the
+    offsets' stands for it (nothing reads it)."""
+    idx, offsets = _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets")
+    return offsets if idx == 0 else idx, offsets
+
+
 def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=None):
     n = seq.numel()
     if kept_offsets.numel() != n + 1:             # move() takes n from it
@@ -330,8 +337,7 @@ def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=
     dev = pages.index
     _enqueue(lib().occam_pages_keep, dev, stream, pages.ref, n, _ints(seq, dev, "seq"),
              _ints(span_start, dev, "span_start", n), _ints(span_len, dev, "span_len", n),
-             _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets"),
-             *_plan(pages, plan))
+             *_lists(kept_idx, kept_offsets, dev), *_plan(pages, plan))
 
 
 # ------------------------------------------------------------------------------- rows
@@ -374,7 +380,7 @@ def move(pages, layer, plan, kept_idx, kept_offsets, stream=None):
     """occam_cache_move with the plan and the lists of :func:`keep`."""
     dev = pages.index
     _enqueue(lib().occam_cache_move, dev, stream, pages.ref, layer.ref, kept_offsets.numel() - 1,
-             *_plan(pages, plan), _ints(kept_idx, dev, "kept_idx"), _ints(kept_offsets, dev, "kept_offsets"))
+             *_plan(pages, plan), *_lists(kept_idx, kept_offsets, dev))
 
 
 # --------------------------------------------------------------------------- attention
