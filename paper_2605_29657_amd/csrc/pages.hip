@@ -66,7 +66,7 @@ struct PlanShared {
 };
 
 // Prefixes of the two numbers that get(i) gives for i in [0, n) into out[0 .. n] each;
-// returns their sums.  (Sums stay below 2^31: a call's rows do.)
+// returns their sums.  (For what follows from a call's rows, which stay below 2^31.)
 struct Two { int a, b; };
 template <int NT, typename F>
 __device__ __forceinline__ Two prefix_of(int n, int* out_a, int* out_b, long long* red, F get) {
@@ -87,6 +87,23 @@ __device__ __forceinline__ Two prefix_of(int n, int* out_a, int* out_b, long lon
         out_b[n] = (int)base;
     }
     return Two{(int)(base >> 32), (int)base};
+}
+
+// Prefixes of the number that get(i) gives for i in [0, n) into out[0 .. n]; returns their sum,
+// which may pass 2^31 (forks share pages: what a call replaces can be many times the pool).
+// The prefixes are right where it does not.
+template <int NT, typename F>
+__device__ __forceinline__ long long wide_prefix_of(int n, int* out, long long* red, F get) {
+    long long base = 0;
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + threadIdx.x;
+        long long total;
+        const long long at = base + block_scan<NT>(i < n ? (long long)get(i) : 0ll, &total, red);
+        if (i < n) out[i] = (int)at;
+        base += total;
+    }
+    if (threadIdx.x == 0) out[n] = (int)base;
+    return base;
 }
 
 // The clear bits of word w of the map that are pages.
@@ -441,10 +458,11 @@ __global__ __launch_bounds__(NT) void keep_plan(PageView p, int n, const int* se
         if (bad) atomicOr(&sh.bad, bad);
     }
     __syncthreads();
-    const int need = prefix_of<NT>(n, sh.need, sh.items, sh.red2, [&](int i) {
+    const long long want = wide_prefix_of<NT>(n, sh.need, sh.red2, [&](int i) {
         const int pages = ((news[i] + G - 1) >> p.shift) - first[i];
-        return Two{sh.bad || pages < 0 ? 0 : pages, 0};
-    }).a;
+        return sh.bad || pages < 0 ? 0 : pages;
+    });
+    const int need = want > p.num_pages ? p.num_pages + 1 : (int)want;     // (more than there can be)
     __syncthreads();
     const bool listed = need <= kList;
     int* list = listed ? sh.list : plan_record(plan, n, p.max_pages, 0);
