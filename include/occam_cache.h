@@ -29,9 +29,13 @@
  * layers) may overlap each other.  Inputs must be finite.
  *
  * What the host cannot check is checked on the device: a slot outside the cache or listed
- * twice, a sequence that would outgrow its table, a pool without enough free pages.  The
- * call then changes nothing at all, its plan is empty (the calls that read the plan do
- * nothing), and a bit of *status is set, which stays until the caller clears it.
+ * twice, a sequence that would outgrow its table, a pool without enough free pages, row
+ * offsets that descend or pass the stated bound.  The call then changes nothing at all, its
+ * plan is empty (the calls that read the plan do nothing), and a bit of *status is set, which
+ * stays until the caller clears it.  occam_cache_read and occam_cache_attend set the bits for
+ * slots and row offsets too, and serve the other sequences of the batch: rows of a slot that
+ * there is not are left alone by the one and get zeros and -infinity from the other, rows of a
+ * sequence whose offsets are wrong are left alone by both.
  *
  * 8-bit values.  A page holds page_tokens tokens of one sequence.  For every page and key
  * head, keys and values have one scale each: the smallest power of two that brings the
@@ -61,7 +65,8 @@ typedef enum {
     OCCAM_PAGES_FULL = 1,     /* not enough free pages                                 */
     OCCAM_PAGES_BAD_SEQ = 2,  /* a slot out of range, listed twice, or (fork) not empty */
     OCCAM_PAGES_TOO_LONG = 4, /* a sequence would need more than max_pages pages       */
-    OCCAM_PAGES_BAD_SPAN = 8  /* keep: a span outside its sequence, or more survivors  */
+    OCCAM_PAGES_BAD_SPAN = 8, /* keep: a span outside its sequence, or more survivors  */
+    OCCAM_PAGES_BAD_ROWS = 16 /* row_offsets that descend, or pass max_rows            */
 } occam_pages_status;
 
 /* The pages of a cache, shared by all its layers.  Device arrays of the caller,
@@ -97,7 +102,8 @@ typedef struct {
     const int32_t *seq;         /* device [n], or NULL                                  */
     int32_t rows;               /* rows per sequence when row_offsets == NULL, >= 1     */
     const int32_t *row_offsets; /* device [n+1], non-decreasing, or NULL                */
-    int32_t max_rows;           /* upper bound of a sequence's rows with row_offsets    */
+    int32_t max_rows;           /* upper bound of a sequence's rows with row_offsets,
+                                   >= 1 (also where no sequence owns a row)             */
 } occam_batch;
 
 /* --------------------------------------------------------------- rotary positions */

@@ -33,7 +33,7 @@ import torch
 from . import occam
 
 HALVES, ADJACENT = 0, 1
-FULL, BAD_SEQ, TOO_LONG, BAD_SPAN = 1, 2, 4, 8     # bits of Pages.status
+FULL, BAD_SEQ, TOO_LONG, BAD_SPAN, BAD_ROWS = 1, 2, 4, 8, 16     # bits of Pages.status
 
 EXPORTS = ("occam_rotary_init", "occam_rotate", "occam_pages_plan_size",
            "occam_cache_storage_size", "occam_pages_reset", "occam_pages_reserve",
@@ -268,7 +268,7 @@ class Layer:
 class Batch:
     """occam_batch: ``n`` sequences (slots ``seq``, or 0 .. n-1) with ``rows`` rows each, or
     with the packed rows that the int32 device prefix ``row_offsets`` ([n+1]) gives them, at
-    most ``max_rows`` each."""
+    most ``max_rows`` each (a bound of at least 1; :data:`BAD_ROWS` where they pass it)."""
 
     def __init__(self, n, rows=1, seq=None, row_offsets=None, max_rows=0):
         self.n, self.seq, self.row_offsets = int(n), seq, row_offsets     # kept alive

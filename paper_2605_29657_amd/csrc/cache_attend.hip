@@ -96,6 +96,14 @@ __device__ __forceinline__ Block block_of(const AttendArgs& a, int entry, int ro
     t.end = a.causal ? t.len - t.T + (last < t.T - 1 ? last : t.T - 1) + 1 : t.len;
     return t;
 }
+// One workgroup, the last, which has little or nothing else to do, looks for slots that there
+// are not and for rows that the offsets give wrongly.
+template <int NT>
+__device__ __forceinline__ void report_faults(const AttendArgs& a) {
+    if (!a.b.seq && !a.b.off) return;
+    for (int i = threadIdx.x; i < a.b.n; i += NT)
+        if (const int bad = batch_faults(a.pg, slot_of(a.b, i), stated_rows(a.b, i))) atomicOr(a.pg.status, bad);
+}
 // Units of keys of a row block: one where there is nothing to see (zeros are written), none
 // where there are no rows.
 __device__ __forceinline__ int units_of(const AttendArgs& a, const Block& t, int unit) {
@@ -251,6 +259,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
     const int w = blockIdx.x / a.c.Hkv, h = blockIdx.x - w * a.c.Hkv;
     const Range range = range_of<64 * kFewWaves>(a, w, ROWS, kFewUnit, 1, red);
     if (a.shape.slots > 0 && h == 0 && threadIdx.x == 0) note_cut(a, range, w, kFewUnit);
+    if (w + 1 == a.shape.ranges && h + 1 == a.c.Hkv) report_faults<64 * kFewWaves>(a);
     int entry = range.entry, at_unit = range.start - range.first;
     for (int now = range.start; now < range.stop && entry < a.b.n * a.shape.blocks; ++entry, at_unit = 0) {
     const Block block = entry == range.entry ? range.block : block_of(a, entry, ROWS);
@@ -648,6 +657,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void attend_many(Att
     const int parts = (units + each - 1) / each;
     if (a.shape.slots > 0 && h == 0 && part == 0 && threadIdx.x == 0)
         a.cuts[entry] = int4{parts > 1 ? entry : -1, parts, entry * a.shape.ranges, 1};
+    if (h + 1 == a.c.Hkv && entry + 1 == a.b.n * a.shape.blocks && part + 1 == a.shape.ranges) report_faults<THREADS>(a);
     if (part >= parts) return;
     const bool whole = parts == 1;
     const int i = block.i, T = block.T, len = block.len, r0 = block.r0;

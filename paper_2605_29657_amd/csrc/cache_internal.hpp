@@ -35,10 +35,21 @@ __device__ __forceinline__ int slot_of(const BatchView& b, int i) { return b.seq
 __device__ __forceinline__ int row_begin(const BatchView& b, int i) {
     return b.off ? b.off[i] : i * b.rows;
 }
-__device__ __forceinline__ int row_count(const BatchView& b, int i) {
+// Rows that the offsets give sequence i, or -1 where they descend or pass the host's bound;
+// such a sequence's rows are left alone.
+__device__ __forceinline__ int stated_rows(const BatchView& b, int i) {
     if (!b.off) return b.rows;
     const int r = b.off[i + 1] - b.off[i];
-    return r < 0 ? 0 : r < b.max_rows ? r : b.max_rows;
+    return r <= b.max_rows ? r < 0 ? -1 : r : -1;
+}
+__device__ __forceinline__ int row_count(const BatchView& b, int i) {
+    const int r = stated_rows(b, i);
+    return r < 0 ? 0 : r;
+}
+// The status bits of a sequence: a slot that there is not, rows that the offsets give wrongly.
+__device__ __forceinline__ int batch_faults(const PageView& p, int slot, int stated) {
+    return (slot < 0 || slot >= p.num_seqs ? (int)OCCAM_PAGES_BAD_SEQ : 0) |
+           (stated < 0 ? (int)OCCAM_PAGES_BAD_ROWS : 0);
 }
 
 // The plan: a header of four ints (kind, n, page items, 0), arrays of n + 1 ints, for keep

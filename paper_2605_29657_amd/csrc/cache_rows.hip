@@ -207,8 +207,11 @@ template <bool F32, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void cache_read(PageView p, CacheView c, BatchView b,
                                                           const int* start, char* k, long long kst,
                                                           char* v, long long vst) {
-    const int i = blockIdx.y, rows = row_count(b, i), s = slot_of(b, i);
-    if (s < 0 || s >= p.num_seqs) return;
+    const int i = blockIdx.y, rows = stated_rows(b, i), s = slot_of(b, i);
+    if (s < 0 || s >= p.num_seqs || rows < 0) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, batch_faults(p, s, rows));
+        return;
+    }
     const int a = start ? start[i] : 0, len = p.length[s];
     const long long last = (long long)a + rows < len ? (long long)a + rows : len;   // past the end
     const int lo = a > 0 ? a : 0;

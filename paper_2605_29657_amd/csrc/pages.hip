@@ -239,13 +239,13 @@ __global__ __launch_bounds__(NT) void pages_reserve(PageView p, BatchView b, int
     int* slot = near ? sh.near[3] : g_slot;
     begin_call<NT>(p, sh.seen, &sh.bad);
     for (int i = threadIdx.x; i < n; i += NT) {
-        const int s = slot_of(b, i), r = row_count(b, i);
-        int bad = 0, len = 0, src = -1;
+        const int s = slot_of(b, i), stated = stated_rows(b, i), r = stated < 0 ? 0 : stated;
+        int bad = stated < 0 ? (int)OCCAM_PAGES_BAD_ROWS : 0, len = 0, src = -1;
         if (bad_slot(p, sh.seen, s)) {
-            bad = OCCAM_PAGES_BAD_SEQ;
+            bad |= OCCAM_PAGES_BAD_SEQ;
         } else {
             len = p.length[s];
-            if ((long long)len + r > ((long long)p.max_pages << p.shift)) bad = OCCAM_PAGES_TOO_LONG;
+            if ((long long)len + r > ((long long)p.max_pages << p.shift)) bad |= OCCAM_PAGES_TOO_LONG;
             else if (r > 0 && (len & (G - 1))) src = p.table[(size_t)s * p.max_pages + (len >> p.shift)];
         }
         first[i] = len;

@@ -1,5 +1,7 @@
 """What the binding of the cache's entry points passes on and what it refuses, without a GPU:
 its tensors lie on the CPU here (device index -1) and nothing is enqueued."""
+import os
+import re
 import types
 
 import pytest
@@ -41,3 +43,10 @@ def test_no_survivor_at_all(calls):
     cache.move(pages(), layer(), two, none, offsets)
     assert calls[0][5] == offsets.data_ptr()
     assert calls[1][5] == offsets.data_ptr() and calls[1][6] == offsets.data_ptr()
+
+
+def test_status_bits_are_the_headers():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "occam_cache.h")).read()
+    bits = {n: int(v) for n, v in re.findall(r"OCCAM_PAGES_([A-Z_]+) = (\d+)", text)}
+    assert bits == {n: getattr(cache, n) for n in ("FULL", "BAD_SEQ", "TOO_LONG", "BAD_SPAN", "BAD_ROWS")}
