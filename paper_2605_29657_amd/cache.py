@@ -370,6 +370,8 @@ def read(pages, layer, batch, k, v=None, start=None, stream=None):
     if v is not None:
         vp, vs, n = _rows(v, dev, "v", layer.num_kv_heads, layer.head_dim, dt)
         batch.check(dev, n)
+        if n != x.shape[0]:
+            _bad("k and v must have the same rows")
     if x.shape[0] == 0:
         return
     _enqueue(lib().occam_cache_read, dev, stream, pages.ref, layer.ref, batch.ref,

@@ -50,3 +50,18 @@ def test_status_bits_are_the_headers():
     text = open(os.path.join(root, "include", "occam_cache.h")).read()
     bits = {n: int(v) for n, v in re.findall(r"OCCAM_PAGES_([A-Z_]+) = (\d+)", text)}
     assert bits == {n: getattr(cache, n) for n in ("FULL", "BAD_SEQ", "TOO_LONG", "BAD_SPAN", "BAD_ROWS")}
+
+
+def ragged(n=2, most=4):
+    return cache.Batch(n, row_offsets=torch.zeros(n + 1, dtype=torch.int32), max_rows=most)
+
+
+def test_read_wants_keys_and_values_of_the_same_rows(calls):
+    k, v = torch.zeros(8, 2, 8), torch.zeros(5, 2, 8)
+    for a, b in ((k, v), (v, k)):
+        with pytest.raises(occam.OccamError, match="same rows"):
+            cache.read(pages(), layer(), ragged(), a, b)
+    assert not calls
+    for a, b in ((k, k.clone()), (k, None), (None, v)):
+        cache.read(pages(), layer(), ragged(), a, b)
+    assert len(calls) == 3
