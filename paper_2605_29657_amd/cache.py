@@ -252,6 +252,7 @@ class Layer:
 
     def __init__(self, pages, num_kv_heads, head_dim):
         self.num_kv_heads, self.head_dim = int(num_kv_heads), int(head_dim)
+        self.num_pages, self.page_tokens, self.index = pages.num_pages, pages.page_tokens, pages.index
         size = lib().occam_cache_storage_size(pages.ref, self.num_kv_heads, self.head_dim)
         if size == 0:
             _bad("invalid layer")
@@ -341,9 +342,16 @@ def keep(pages, seq, span_start, span_len, kept_idx, kept_offsets, plan, stream=
 
 
 # ------------------------------------------------------------------------------- rows
+def _layer(pages, layer):
+    """The device of the pages, whose numbers the layer has storage for."""
+    if layer.num_pages < pages.num_pages or layer.page_tokens != pages.page_tokens or layer.index != pages.index:
+        _bad("the layer must have been made for these pages")
+    return pages.index
+
+
 def append(pages, layer, batch, plan, k, v, stream=None):
     """occam_cache_append: ``k`` and ``v`` [rows, num_kv_heads, head_dim], float32 or bfloat16."""
-    dev, dt = pages.index, k.dtype
+    dev, dt = _layer(pages, layer), k.dtype
     if dt not in _DTYPES:
         _bad("k and v must be float32 or bfloat16 tensors")
     kp, ks, n = _rows(k, dev, "k", layer.num_kv_heads, layer.head_dim, dt)
@@ -359,7 +367,7 @@ def append(pages, layer, batch, plan, k, v, stream=None):
 
 def read(pages, layer, batch, k, v=None, start=None, stream=None):
     """occam_cache_read into ``k`` and ``v`` (either may be None), float32 or bfloat16."""
-    dev = pages.index
+    dev = _layer(pages, layer)
     x = k if k is not None else v
     if x is None or x.dtype not in _DTYPES:
         _bad("k or v must be a float32 or bfloat16 tensor")
@@ -380,7 +388,7 @@ def read(pages, layer, batch, k, v=None, start=None, stream=None):
 
 def move(pages, layer, plan, kept_idx, kept_offsets, stream=None):
     """occam_cache_move with the plan and the lists of :func:`keep`."""
-    dev = pages.index
+    dev = _layer(pages, layer)
     _enqueue(lib().occam_cache_move, dev, stream, pages.ref, layer.ref, kept_offsets.numel() - 1,
              *_plan(pages, plan), *_lists(kept_idx, kept_offsets, dev))
 
@@ -403,12 +411,12 @@ def attend(pages, layer, batch, q, out, ws, lse=None, causal=True, softmax_scale
            stream=None):
     """occam_cache_attend: ``q`` and ``out`` bfloat16 [rows, num_heads, head_dim], ``lse``
     float32 [rows, num_heads] or None.  ``q`` and ``out`` must not overlap."""
-    dev, H = pages.index, q.shape[1] if q.dim() == 3 else 0
+    dev, H = _layer(pages, layer), q.shape[1] if q.dim() == 3 else 0
     qp, qs, n = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)
     op, os, m = _rows(out, dev, "out", H, layer.head_dim, torch.bfloat16)
     batch.check(dev, n)
-    if n != m or ws.get_device() != dev:
-        _bad("q and out must have the same rows, and the workspace the pages' device")
+    if n != m or ws.get_device() != dev or not ws.is_contiguous():
+        _bad("q and out must have the same rows, and the workspace be contiguous on the pages' device")
     if lse is not None and (lse.dtype is not _F32 or lse.get_device() != dev or not lse.is_contiguous() or
                             lse.numel() < n * H):
         _bad("lse must be a contiguous float32 tensor [rows, %d] on GPU %s" % (H, dev))

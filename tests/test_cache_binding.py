@@ -65,3 +65,34 @@ def test_read_wants_keys_and_values_of_the_same_rows(calls):
     for a, b in ((k, k.clone()), (k, None), (None, v)):
         cache.read(pages(), layer(), ragged(), a, b)
     assert len(calls) == 3
+
+
+@pytest.mark.parametrize("kw", [dict(num_pages=7), dict(page_tokens=32), dict(index=1)])
+def test_a_layer_of_other_pages(calls, kw):
+    # Its storage has fewer pages, other ones, or lies on another GPU.
+    p, c, b = pages(), layer(**kw), cache.Batch(1, rows=3)
+    x, plan, idx, ws = torch.zeros(3, 2, 8), i32(0), i32(0, 1), torch.zeros(64, dtype=torch.uint8)
+    q = torch.zeros(3, 2, 8, dtype=torch.bfloat16)
+    for call in (lambda: cache.append(p, c, b, plan, x, x), lambda: cache.read(p, c, b, x),
+                 lambda: cache.move(p, c, plan, idx, idx), lambda: cache.attend(p, c, b, q, q.clone(), ws)):
+        with pytest.raises(occam.OccamError, match="layer"):
+            call()
+    assert not calls
+
+
+def test_a_layer_of_its_pages_or_of_more(calls):
+    b, x = cache.Batch(1, rows=3), torch.zeros(3, 2, 8)
+    for c in (layer(), layer(num_pages=9)):
+        cache.append(pages(), c, b, i32(0), x, x)
+        cache.read(pages(), c, b, x)
+        cache.move(pages(), c, i32(0), i32(0), i32(0, 1))
+        cache.attend(pages(), c, b, x.bfloat16(), x.bfloat16(), torch.zeros(64, dtype=torch.uint8))
+    assert len(calls) == 8
+
+
+def test_the_workspace_is_one_piece(calls):
+    b, q = cache.Batch(1, rows=3), torch.zeros(3, 2, 8, dtype=torch.bfloat16)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(64, dtype=torch.uint8)[::2]):
+        with pytest.raises(occam.OccamError, match="workspace"):
+            cache.attend(pages(), layer(), b, q, q.clone(), ws)
+    assert not calls
