@@ -118,7 +118,8 @@ typedef struct {
 
 /* One tensor of rows to rotate: [rows][heads][head_dim], heads packed, rows stride apart
  * (in elements, >= heads * head_dim).  dst may be src (in place); otherwise they must not
- * overlap. */
+ * overlap, and no tensor's dst may overlap another one's src or dst (rows that interleave, as
+ * slices of one projection do, must be equally far apart). */
 typedef struct {
     const void *src;
     void *dst;

@@ -121,6 +121,18 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     return OCCAM_OK;
 }
 
+// Whether rows of `wa` and `wb` bytes, the first at a and b, `sa` and `sb` bytes apart, overlap.
+// Rows as far apart as each other may interleave (slices of one projection); of rows otherwise
+// apart those whose ranges meet count as overlapping.
+bool rows_meet(uintptr_t a, long long sa, long long wa, uintptr_t b, long long sb, long long wb, int rows) {
+    if (b < a) return rows_meet(b, sb, wb, a, sa, wa, rows);
+    const long long gap = (long long)(b - a);
+    if (rows < 1 || gap >= (rows - 1) * sa + wa) return false;
+    if (rows == 1 || sa != sb) return true;
+    const long long in = gap % sa;
+    return in < wa || in + wb > sa;
+}
+
 // The largest power of two up to `most` that divides x.
 int pow2_in(long long x, int most) {
     const long long low = x & -x;
@@ -182,18 +194,17 @@ occam_status occam_rotate(const occam_rotary* rotary, int32_t rows, const int32_
             (t.src == t.dst && t.src_row_stride != t.dst_row_stride))
             return OCCAM_ERR_INVALID_ARG;
         const uintptr_t s0 = reinterpret_cast<uintptr_t>(t.src), d0 = reinterpret_cast<uintptr_t>(t.dst);
-        if (rows > 0 && s0 != d0) {
-            // Ranges that interleave (strided views of one tensor) do not overlap in rows
-            // that are both given, so only a partial overlap within a row is refused.
-            const long long st = t.src_row_stride * e;
-            const long long gap = s0 < d0 ? (long long)(d0 - s0) : (long long)(s0 - d0);
-            const long long span_s = (rows - 1) * st + row * e;
-            const long long span_d = (rows - 1) * t.dst_row_stride * e + row * e;
-            if (gap < (s0 < d0 ? span_s : span_d)) {
-                if (t.src_row_stride != t.dst_row_stride) return OCCAM_ERR_INVALID_ARG;
-                const long long in = gap % st;
-                if (in < row * e || st - in < row * e) return OCCAM_ERR_INVALID_ARG;
-            }
+        const long long ss = t.src_row_stride * e, ds = t.dst_row_stride * e;
+        if (s0 != d0 && rows_meet(s0, ss, row * e, d0, ds, row * e, rows)) return OCCAM_ERR_INVALID_ARG;
+        // Nor does anything that one tensor writes lie in another one's rows.
+        for (int j = 0; j < i; ++j) {
+            const RotTensor& o = a.t[j];
+            const uintptr_t os = reinterpret_cast<uintptr_t>(o.src), od = reinterpret_cast<uintptr_t>(o.dst);
+            const long long ow = (long long)o.heads * r.head_dim * e;
+            if (rows_meet(d0, ds, row * e, od, o.dst_stride, ow, rows) ||
+                (os != od && rows_meet(d0, ds, row * e, os, o.src_stride, ow, rows)) ||
+                (s0 != d0 && rows_meet(s0, ss, row * e, od, o.dst_stride, ow, rows)))
+                return OCCAM_ERR_INVALID_ARG;
         }
         heads += t.heads;
         vec = pow2_in((long long)(s0 / e) | (long long)(d0 / e), vec);
