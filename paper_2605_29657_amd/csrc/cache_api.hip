@@ -110,6 +110,9 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
         return OCCAM_ERR_UNSUPPORTED;
     const AttendShape& x = a.shape = attend_shape(c, b, a.H, most);
     if (x.cuts > 65535) return OCCAM_ERR_UNSUPPORTED;      // a launch's grid.y
+    // A launch has fewer than 2^32 threads: of the many-row form, two for every row of its blocks.
+    if (!x.few && (double)b.n * x.blocks * x.ranges * c.Hkv * (2 * x.block_rows) >= 4294967296.0)
+        return OCCAM_ERR_UNSUPPORTED;
     if (x.slots > 0) {
         const size_t rows = (size_t)c.Hkv * x.slots * x.block_rows;
         out->off_l = align_up(rows * c.dp * sizeof(float));

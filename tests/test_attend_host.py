@@ -1,0 +1,31 @@
+"""Attention arguments that no launch can hold, refused by the host (no call here reaches one)."""
+import os
+
+import pytest
+
+from paper_2605_29657_amd import build as occam_build
+from paper_2605_29657_amd import cache, occam
+
+FAKE = 0x7f0000000000
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(occam.LIB_PATH):
+        occam_build.build()
+    return cache.lib()
+
+
+def refused(L, status, n, rows, H, Hkv, **kw):
+    p = cache._Pages(64, 64, 8192, 4, FAKE, FAKE, FAKE, FAKE, FAKE)
+    c = cache._Cache(Hkv, 8, FAKE, FAKE, FAKE, FAKE)
+    b = cache._Batch(n, None, rows, None, 0)
+    a = cache._Attention(**dict(dict(num_heads=H, causal=1, softmax_scale=0.0, max_tokens=0), **kw))
+    return L.occam_cache_workspace_size(p, c, b, a) == 0 and L.occam_cache_attend(
+        p, c, b, a, FAKE, 8 * H, FAKE + (1 << 40), 8 * H, None, FAKE, 1 << 50, None) == status
+
+
+@pytest.mark.parametrize("n,rows,H,Hkv", [(8192, 33, 2048, 2048), (8192, 129, 1024, 1024), (4096, 200, 2500, 2500)])
+def test_more_workgroups_than_a_launch_holds(L, n, rows, H, Hkv):
+    # 2^32 threads and more, by row blocks that their rows fill badly.
+    assert refused(L, occam.ERR_UNSUPPORTED, n, rows, H, Hkv)
