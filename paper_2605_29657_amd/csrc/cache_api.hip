@@ -101,6 +101,7 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     a.causal = at->causal;
     const float scale = at->softmax_scale > 0.f ? at->softmax_scale : 1.0f / sqrtf((float)c.d);
     a.scale2 = scale * kLog2e;
+    if (isinf(a.scale2)) return OCCAM_ERR_INVALID_ARG;
     const long long cap = (long long)p.max_pages << p.shift;
     const long long most = at->max_tokens && at->max_tokens < cap ? at->max_tokens : cap;
     // (row, head) pairs are numbered in 32 bits, and so are row blocks.

@@ -29,3 +29,8 @@ def refused(L, status, n, rows, H, Hkv, **kw):
 def test_more_workgroups_than_a_launch_holds(L, n, rows, H, Hkv):
     # 2^32 threads and more, by row blocks that their rows fill badly.
     assert refused(L, occam.ERR_UNSUPPORTED, n, rows, H, Hkv)
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_a_scale_past_float32_in_base_2(L, scale):
+    assert refused(L, occam.ERR_INVALID_ARG, 4, 1, 8, 2, softmax_scale=scale)
