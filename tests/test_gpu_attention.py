@@ -153,6 +153,31 @@ def test_outputs_do_not_depend_on_hidden_tokens():
     assert torch.equal(outs[0][0][:32], outs[1][0][:32]) and torch.equal(outs[0][1], outs[1][1])
 
 
+# ------------------------------------------------------------------- many keys in one part
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page,H,Hkv,d,T,n", [(16, 16, 8, 64, 40, 64), (64, 8, 8, 128, 128, 64), (16, 8, 8, 128, 47, 64),
+                                              (16, 16, 8, 256, 50, 32), (32, 16, 8, 128, 90, 32), (16, 32, 8, 80, 70, 16)])
+def test_many_rows_over_many_keys_in_one_part(page, H, Hkv, d, T, n, causal):
+    # As many row blocks as the chip holds, so that none is cut: a workgroup passes more keys
+    # than the 1024 whose pages it has at hand, and again.  The sequences are forks of two.
+    c = Cache(n, page, Hkv, d, num_pages=8000 // page + 9, max_pages=5100 // page, seed=T)
+    lens = [2500 + page // 2 + 3, 4999]
+    c.append([0, 1], lens)
+    rest = list(range(2, n))
+    c.fork([s % 2 for s in rest], rest)
+    q = torch.randn(4, T, H, d, generator=c.gen, device=DEV).bfloat16()
+    which = [s % 4 for s in range(n)]                             # slots 0 to 3 with a query each
+    b = cache.Batch(n, rows=T)
+    ws = cache.workspace(c.pages, c.layer, b, H, max(lens))
+    out = torch.empty(n, T, H, d, device=DEV, dtype=torch.bfloat16)
+    lse = torch.empty(n, T, H, device=DEV)
+    cache.attend(c.pages, c.layer, b, q[which].flatten(0, 1), out.flatten(0, 1), ws, lse=lse.flatten(0, 1),
+                 causal=causal, max_tokens=max(lens))
+    assert torch.equal(out, out[which]) and torch.equal(lse, lse[which])
+    for s in range(4):
+        A.check(M.f64(out[s]), M.f64(lse[s]), M.f64(q[s]), c.k[s].x, c.v[s].x, A.per_token(c.v[s]), causal)
+
+
 # ------------------------------------------------------- the attention tests of test_gpu_cache
 # Once more, where outputs that are no numbers fail them.
 from test_gpu_cache import (test_attend, test_attend_17_to_32_rows_in_one_block,                # noqa: E402,F401

@@ -98,3 +98,89 @@ def test_reading_calls_say_which_slots_there_are_not(n, T):
     unchanged(c, was, cache.BAD_SEQ)
     assert (out[T:] == 0).all() and (lse[T:] == -np.inf).all()
     M.check_attention(M.f64(out[:T]), M.f64(lse[:T]), M.f64(q[:T]), c.k[0].x, c.v[0].x, True)
+
+
+# ------------------------------------------------------------- calls past a launch's workgroups
+def fill(c, slots, rows, k, v, together):
+    """Appends ``rows`` tokens each to ``slots`` (their keys and values packed), in one call or
+    one call each: the same pages either way."""
+    at = prefix(rows)
+    for part in ([range(len(slots))] if together else [[x] for x in range(len(slots))]):
+        b = c.batch([slots[x] for x in part], [rows[x] for x in part])
+        cache.reserve(c.pages, b, c.plan)
+        x = slice(at[part[0]], at[part[-1] + 1])
+        cache.append(c.pages, c.layer, b, c.plan, k[x], v[x])
+
+
+def values(c, slots, lens):
+    k, v = (torch.empty(sum(lens), c.Hkv, c.d, device=DEV) for _ in range(2))
+    for s, a, n in zip(slots, prefix(lens), lens):               # one by one: small calls
+        cache.read(c.pages, c.layer, cache.Batch(1, rows=n, seq=i32([s])), k[a:a + n], v[a:a + n])
+    return k, v
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page,Hkv,d,tokens", [(64, 8, 128, 50000), (16, 64, 64, 12000), (128, 8, 128, 95000),
+                                               (256, 16, 128, 46000), (256, 8, 256, 90000), (32, 12, 128, 32000)])
+def test_more_blocks_than_workgroups(page, Hkv, d, tokens, dtype):
+    # Appending and moving walk their blocks with 4096 workgroups at most: in one call here,
+    # against small calls (which the other tests compare with the model), bit for bit.
+    n = 5
+    lens = [tokens // 8, tokens // 4 + 3, 7, tokens // 2 - 11, tokens // 8 + 1]
+    num = sum(lens) // page + 4 * n
+    units = page * (8 if d <= 64 else 16 if d <= 128 else 32) // 4
+    side, heads = max(256 // units, 1), 2 if units <= 512 else 1         # blocks and heads of a workgroup
+    fresh = sum(-(-x * 3 // 4 // page) for x in lens)
+    assert sum(lens) // page * Hkv * 2 > 4096 * side and fresh * (Hkv // heads) * 2 > 4096 * side
+    r = np.random.default_rng(page + d)
+    cs = [Cache(n, page, Hkv, d, num_pages=2 * num, max_pages=num, seed=1, dtype=dtype) for _ in range(2)]
+    g = torch.Generator(device=DEV).manual_seed(d)
+    size = torch.exp2(torch.randint(-8, 9, (sum(lens), 1, 1), generator=g, device=DEV).float())
+    for rows, z in ((lens, size), ([5, 1, 2, page, 3], 300.0)):   # the second raises most pages' scales
+        k, v = (torch.randn(sum(rows), Hkv, d, generator=g, device=DEV).mul_(z).to(dtype) for _ in range(2))
+        for c, together in zip(cs, (True, False)):
+            fill(c, list(range(n)), rows, k, v, together)
+    a, b = cs
+    for x, y in ((a.pages.table, b.pages.table), (a.pages.length, b.pages.length), (a.layer.k, b.layer.k),
+                 (a.layer.v, b.layer.v), (a.layer.k_scale.view(torch.int32), b.layer.k_scale.view(torch.int32)),
+                 (a.layer.v_scale.view(torch.int32), b.layer.v_scale.view(torch.int32))):
+        assert torch.equal(x, y)
+    lens = a.pages.length.tolist()
+    kept = [np.sort(r.choice(x, x * 3 // 4, replace=False)) for x in lens]
+    for c, together in zip(cs, (True, False)):
+        for part in ([range(n)] if together else [[x] for x in range(n)]):
+            idx = i32(np.concatenate([kept[x] for x in part]))
+            offs = i32(prefix([len(kept[x]) for x in part]))
+            cache.keep(c.pages, i32(part), i32([0] * len(part)), i32([lens[x] for x in part]), idx, offs, c.plan)
+            cache.move(c.pages, c.layer, c.plan, idx, offs)
+        assert c.pages.status.item() == 0
+    lens = [len(x) for x in kept]
+    assert a.pages.length.tolist() == b.pages.length.tolist() == lens
+    for x, y in zip(values(a, range(n), lens), values(b, range(n), lens)):
+        assert torch.equal(x, y)
+    k, v = (torch.empty(sum(lens), Hkv, d, device=DEV) for _ in range(2))              # and read in one call
+    cache.read(a.pages, a.layer, a.batch(list(range(n)), lens), k, v)
+    for x, y in zip((k, v), values(a, range(n), lens)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page,Hkv,d", [(64, 8, 128), (16, 3, 80), (128, 5, 256)])
+def test_reading_more_than_the_caches_hold(page, Hkv, d, dtype):
+    # Past 256 MB, outputs go past the caches: against parts, bit for bit, and rows behind the
+    # sequences' ends stay.
+    n = (300 << 20) // (2 * Hkv * d * dtype.itemsize)
+    lens = [n // 3, n - n // 3 - 5]
+    c = Cache(2, page, Hkv, d, num_pages=n // page + 4, max_pages=n // page + 2)
+    k, v = (torch.randn(n, Hkv, d, generator=c.gen, device=DEV).bfloat16() for _ in range(2))
+    fill(c, [0, 1], lens, k, v, True)
+    rows = [lens[0] + 2, lens[1] + 3]
+    k, v = (torch.full((n, Hkv, d), 9.0, device=DEV, dtype=dtype) for _ in range(2))
+    cache.read(c.pages, c.layer, c.batch([0, 1], rows), k, v)
+    wk, wv = (torch.full((n, Hkv, d), 9.0, device=DEV, dtype=dtype) for _ in range(2))
+    for s, a in ((0, 0), (1, rows[0])):
+        for x in range(0, lens[s], 9973):
+            m = min(9973, lens[s] - x)
+            cache.read(c.pages, c.layer, cache.Batch(1, rows=m, seq=i32([s])), wk[a + x:a + x + m], wv[a + x:a + x + m],
+                       start=i32([x]))
+    assert torch.equal(k, wk) and torch.equal(v, wv)

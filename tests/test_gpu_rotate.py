@@ -50,3 +50,25 @@ def test_positions_of_every_size(dtype):
     z = torch.empty_like(x)
     cache.rotate(rot, -pos[:7], [x[:7]], [z[:7]], inverse=True)          # the same turn
     check_rotated(z[:7], x[:7], pos[:7], [0] * 8, freq, False, False)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype,d,pairs,heads,adjacent", [(torch.bfloat16, 128, 64, [14, 3], False),
+                                                          (torch.bfloat16, 128, 32, [12, 8], True),
+                                                          (torch.float32, 72, 36, [16, 16], False),
+                                                          (torch.float32, 256, 128, [3, 2, 1], False)])
+def test_more_rows_than_the_caches_hold(dtype, d, pairs, heads, adjacent, in_place):
+    # Past 256 MB tensors go past the caches: against the same rows in parts, bit for bit.
+    rows = (300 << 20) // (sum(heads) * d * dtype.itemsize)
+    g = torch.Generator(device=DEV).manual_seed(d)
+    pos = torch.randint(-9000, 9000, (rows, 3), generator=g, device=DEV, dtype=torch.int32)
+    rot = cache.Rotary(d, [1e6 ** (-p / pairs) for p in range(pairs)], [p % 3 for p in range(pairs)], 3, adjacent)
+    xs = [torch.randn(rows, h, d, generator=g, device=DEV).to(dtype) for h in heads]
+    want = [torch.empty_like(x) for x in xs]
+    for a in range(0, rows, 20011):
+        z = slice(a, min(a + 20011, rows))
+        cache.rotate(rot, pos[z], [x[z] for x in xs], [y[z] for y in want])
+    out = xs if in_place else [torch.empty_like(x) for x in xs]
+    cache.rotate(rot, pos, xs, None if in_place else out)
+    for x, y in zip(out, want):
+        assert torch.equal(x, y)
