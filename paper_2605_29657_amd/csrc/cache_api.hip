@@ -82,6 +82,18 @@ bool rows_ok(const void* x, long long stride, const CacheView& c, int dtype) {
     return aligned(x, 16) && stride >= (long long)c.Hkv * c.d && stride % per == 0;
 }
 
+// Whether rows of `wa` and `wb` bytes, the first at a and b, `sa` and `sb` bytes apart, overlap.
+// Rows as far apart as each other may interleave (slices of one projection); of rows otherwise
+// apart those whose ranges meet count as overlapping.
+bool rows_meet(uintptr_t a, long long sa, long long wa, uintptr_t b, long long sb, long long wb, int rows) {
+    if (b < a) return rows_meet(b, sb, wb, a, sa, wa, rows);
+    const long long gap = (long long)(b - a);
+    if (rows < 1 || gap >= (rows - 1) * sa + wa) return false;
+    if (rows == 1 || sa != sb) return true;
+    const long long in = gap % sa;
+    return in < wa || in + wb > sa;
+}
+
 struct AttendPlan {
     AttendArgs a;
     size_t off_l, off_cuts, total;
@@ -123,18 +135,6 @@ occam_status attend_plan(const PageView& p, const CacheView& c, const BatchView&
     if (x.ordered) out->total = align_up(x.ordered * sizeof(AttendBlock));     // (then nothing is cut)
     if (out->total < kAlign) out->total = kAlign;
     return OCCAM_OK;
-}
-
-// Whether rows of `wa` and `wb` bytes, the first at a and b, `sa` and `sb` bytes apart, overlap.
-// Rows as far apart as each other may interleave (slices of one projection); of rows otherwise
-// apart those whose ranges meet count as overlapping.
-bool rows_meet(uintptr_t a, long long sa, long long wa, uintptr_t b, long long sb, long long wb, int rows) {
-    if (b < a) return rows_meet(b, sb, wb, a, sa, wa, rows);
-    const long long gap = (long long)(b - a);
-    if (rows < 1 || gap >= (rows - 1) * sa + wa) return false;
-    if (rows == 1 || sa != sb) return true;
-    const long long in = gap % sa;
-    return in < wa || in + wb > sa;
 }
 
 // The largest power of two up to `most` that divides x.
@@ -387,8 +387,12 @@ occam_status occam_cache_attend(const occam_pages* pages, const occam_cache* cac
         q_row_stride % 8 || out_row_stride % 8 || (row_lse && !aligned(row_lse, 4)))
         return OCCAM_ERR_INVALID_ARG;
     if (ws_bytes < ap.total) return OCCAM_ERR_WORKSPACE;
-    // In place would not do: a row's queries are read by several workgroups.
-    if (!given(workspace, kAlign) || q == out) return OCCAM_ERR_INVALID_ARG;
+    // In place would not do: a row's queries are read by several workgroups.  (How many rows
+    // there are is known here without row_offsets only.)
+    if (!given(workspace, kAlign) || q == out ||
+        (!b.off && rows_meet(reinterpret_cast<uintptr_t>(q), q_row_stride * 2, row * 2,
+                             reinterpret_cast<uintptr_t>(out), out_row_stride * 2, row * 2, b.n * b.rows)))
+        return OCCAM_ERR_INVALID_ARG;
     AttendArgs& a = ap.a;
     a.q = static_cast<const unsigned short*>(q);
     a.out = static_cast<unsigned short*>(out);

@@ -34,3 +34,20 @@ def test_more_workgroups_than_a_launch_holds(L, n, rows, H, Hkv):
 @pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
 def test_a_scale_past_float32_in_base_2(L, scale):
     assert refused(L, occam.ERR_INVALID_ARG, 4, 1, 8, 2, softmax_scale=scale)
+
+
+@pytest.mark.parametrize("rows", [1, 5])
+@pytest.mark.parametrize("n", [1, 3])
+def test_queries_and_outputs_that_overlap(L, n, rows):
+    # Of uniform rows, of which the host knows how many there are.
+    p = cache._Pages(64, 64, 8, 16, FAKE, FAKE, FAKE, FAKE, FAKE)
+    c, b = cache._Cache(2, 128, FAKE, FAKE, FAKE, FAKE), cache._Batch(n, None, rows, None, 0)
+    a, row = cache._Attention(8, 1, 0.0, 0), 8 * 128
+    size = L.occam_cache_workspace_size(p, c, b, a)
+    for stride in (row, row + 256):
+        for shift in (0, 256, 2 * row - 16, -256, (n * rows - 1) * stride * 2 + 2 * row - 16):
+            assert L.occam_cache_attend(p, c, b, a, FAKE, stride, FAKE + shift, stride, None, FAKE + (1 << 40), size,
+                                        None) == occam.ERR_INVALID_ARG, (stride, shift)
+    if n * rows > 1:
+        assert L.occam_cache_attend(p, c, b, a, FAKE, row, FAKE + 2 * row, 2 * row, None, FAKE + (1 << 40), size,
+                                    None) == occam.ERR_INVALID_ARG

@@ -178,6 +178,20 @@ def test_many_rows_over_many_keys_in_one_part(page, H, Hkv, d, T, n, causal):
         A.check(M.f64(out[s]), M.f64(lse[s]), M.f64(q[s]), c.k[s].x, c.v[s].x, A.per_token(c.v[s]), causal)
 
 
+@pytest.mark.parametrize("T", [1, 3, 50])
+def test_queries_and_outputs_as_slices_of_one_tensor(T):
+    c = Cache(2, 32, 2, 64)
+    c.append([0, 1], [70, 99])
+    H = 4
+    both = torch.randn(2 * T, 2 * H, 64, generator=c.gen, device=DEV).bfloat16()
+    q, out = both[:, H:], both[:, :H]
+    want, b = torch.empty(2 * T, H, 64, device=DEV, dtype=torch.bfloat16), cache.Batch(2, rows=T)
+    ws = cache.workspace(c.pages, c.layer, b, H)
+    cache.attend(c.pages, c.layer, b, q.contiguous(), want, ws)
+    cache.attend(c.pages, c.layer, b, q, out, ws)
+    assert torch.equal(out, want)
+
+
 # ------------------------------------------------------- the attention tests of test_gpu_cache
 # Once more, where outputs that are no numbers fail them.
 from test_gpu_cache import (test_attend, test_attend_17_to_32_rows_in_one_block,                # noqa: E402,F401
