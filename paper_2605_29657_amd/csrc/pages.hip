@@ -18,13 +18,16 @@ namespace occam {
 namespace {
 
 // Workgroups of the planning kernels: 256 threads for calls of up to 256 sequences and, where
-// the host knows a bound, kSmallPages pages (fewer waves at every barrier), 1024 beyond: 1300
-// pages of 32 sequences take 11.5 us against 13.8, one page each 9.6 against 6.6.
+// the host knows a bound, kSmallPages pages (fewer waves at every barrier), 1024 beyond.
+// Reserving, one call's time between events, with 256 and 1024 threads: 32 sequences of one page
+// 8.8 and 10.7 us, of 8 pages 9.1 and 11.0, 16: 11.1 and 11.2, 31: 15.2 and 11.7, 60: 22.8 and
+// 14.0; 128 of 4: 11.6 and 11.4; one of 512: 10.0 and 10.5, of 1000: 12.8 and 10.9.
 // What a call reads again of its sequences is kept in LDS for up to kNear of them, in the plan
 // beyond; the pages it takes for up to kList of them.
-constexpr int kSmallPages = 1024, kNear = 1024, kList = 4096;
-// Table entries of a fork call that one workgroup of 1024 threads copies by itself: 6.2 us
-// for 32 x 73 entries against 7.6 us in two launches, 7.7 against 8.0 us for 64 x 46.
+constexpr int kSmallPages = 512, kNear = 1024, kList = 4096;
+// Table entries of a fork call that one workgroup of 1024 threads copies by itself: between
+// events, in one and in two launches, 32 tables of 64 entries 7.2 and 9.2 us, of 127 9.0 and 9.6,
+// of 250 11.7 and 9.3; 8 of 512 8.7 and 9.6, of 1000 11.3 and 10.3; 1000 of 4 9.4 and 9.2.
 constexpr int kSmallTables = 4096;
 
 // Exclusive prefix of x over the workgroup (NT threads), and the total.
