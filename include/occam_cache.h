@@ -217,7 +217,8 @@ typedef struct {
     int32_t num_heads;    /* H, a multiple of Hkv; head h reads key head h / (H / Hkv)   */
     int32_t causal;       /* 1: row t of T sees keys 0 .. len - T + t; 0: all len keys   */
     float softmax_scale;  /* 0 => 1/sqrt(d)                                              */
-    int32_t max_tokens;   /* upper bound of the sequences' lengths (0: max_pages * page_tokens) */
+    int32_t max_tokens;   /* upper bound of the sequences' lengths (0: max_pages * page_tokens);
+                             the nearer, the better the form that the call takes         */
 } occam_attention;
 
 /* Bytes of device workspace that occam_cache_attend with the same arguments may use (0 for
@@ -234,8 +235,9 @@ size_t occam_cache_workspace_size(const occam_pages *pages, const occam_cache *c
  * key gets zeros and -infinity.  Probabilities are rounded to float16 (2^-11 of them), sums are
  * float32; a key whose weight (its probability times its block's scale) is far below the row's
  * largest one adds its share to within 2^-26 of that weight.  q and out must not overlap.
- * max_tokens only sizes the launch and the workspace; a longer sequence is still attended to in
- * full. */
+ * max_tokens sizes the launch and the workspace and chooses between forms for few and for many
+ * codes (without a near bound, short sequences in long tables can take a quarter longer); a
+ * longer sequence is still attended to in full. */
 occam_status occam_cache_attend(const occam_pages *pages, const occam_cache *cache,
                                 const occam_batch *batch, const occam_attention *attention,
                                 const void *q, int64_t q_row_stride, void *out,

@@ -15,7 +15,7 @@ A serving step::
     for layer in layers:
         cache.rotate(rotary, positions, [q, k])       # in place
         cache.append(pages, layer, batch, plan, k, v)
-        cache.attend(pages, layer, batch, q, out, ws, lse=row_lse)
+        cache.attend(pages, layer, batch, q, out, ws, lse=row_lse, max_tokens=longest)
 
 and after ``occam.prune`` has chosen a sequence's survivors::
 
@@ -410,7 +410,9 @@ def workspace(pages, layer, batch, num_heads, max_tokens=0):
 def attend(pages, layer, batch, q, out, ws, lse=None, causal=True, softmax_scale=0.0, max_tokens=0,
            stream=None):
     """occam_cache_attend: ``q`` and ``out`` bfloat16 [rows, num_heads, head_dim], ``lse``
-    float32 [rows, num_heads] or None.  ``q`` and ``out`` must not overlap."""
+    float32 [rows, num_heads] or None.  ``q`` and ``out`` must not overlap.  ``max_tokens``: a
+    bound of the lengths (0: what the tables hold), as for :func:`workspace`; a near one lets
+    the call choose the faster form."""
     dev, H = _layer(pages, layer), q.shape[1] if q.dim() == 3 else 0
     qp, qs, n = _rows(q, dev, "q", H, layer.head_dim, torch.bfloat16)
     op, os, m = _rows(out, dev, "out", H, layer.head_dim, torch.bfloat16)

@@ -227,10 +227,10 @@ __device__ __forceinline__ void note_cut(const AttendArgs& a, const Range& r, in
 // Few rows: 16 rows of one key head at a time (or 32: NR = 2), their keys dealt to the
 // workgroup's four waves in steps of 32, joined in LDS.  Bound by reading the codes once: a wave
 // has the loads of two steps in flight (8 KB each at d = 128) and several workgroups share a CU.
-// One row of each of 8 sequences of 16640 tokens, 32 key heads of 128: 175 us, 6.2 TB/s (a
-// large read reaches 5.7); of 64 sequences of 272 to 4608 tokens, 8 key heads: 55 us, 5.2
-// TB/s, about 8 us of it before the first codes arrive (rows, lengths, pages, codes: four
-// loads one after the other); of one sequence of 3011 tokens: 8 us, nothing but latency.
+// One row of each of 8 sequences of 16640 tokens, 32 key heads of 128: 174 us, 6.3 TB/s; of 64
+// sequences of 272 to 4608 tokens, 8 key heads: 54 us, 5.2 TB/s, about 8 us of it before the
+// first codes arrive (rows, lengths, pages, codes: four loads one after the other); of one
+// sequence of 3011 tokens: 7 us, nothing but latency.  Scales past the spread change none of them.
 // ---------------------------------------------------------------------------------------
 constexpr int kStep = 32, kFewWaves = 4, kFewRows = 16;
 constexpr int kFewUnit = kStep * kFewWaves;
@@ -564,11 +564,13 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(DP, NR)) void attend_f
 //
 // What bounds it is the issue of vector instructions beside the matrix core (the products of a
 // tile would take 2100 clocks of a SIMD, the 290 other instructions of its two waves about as
-// many) and the card's power: the prompt below takes 274 us on constant data, at a higher clock,
-// as a large library product gains 28 % there.  A causal prompt of 4 x 3012 tokens, 32 heads of
-// 128: 326 us, 912 TFLOP/s (large library products 1342 to 1415); 16 to 512 text rows of 32
-// images each, behind 256 to 4096 tokens, 32 heads on 8: 246 us, 901 TFLOP/s.  4 x 3000 tokens
-// with 32 heads of 64: 691 TFLOP/s, with 16 of 256: 749.
+// many) and the card's power: the prompt below takes 281 us on constant data, at a higher clock,
+// as a large library product gains 28 % there.  In a long run (the first dispatches after idle
+// take a tenth longer) a causal prompt of 4 x 3012 tokens, 32 heads of 128: 328 us, 906 TFLOP/s
+// (large library products 1371 to 1398), all keys for every row 563 us, 1056; 16 to 512 text rows
+// of 32 images each, behind 256 to 4096 tokens, 32 heads on 8: 243 us, 913 TFLOP/s.  4 x 3000
+// tokens with 32 heads of 64: 738 TFLOP/s, with 16 of 256: 727.  The loop for scales past the
+// spread fetches a tile at a time: 523 us for the prompt.
 // ---------------------------------------------------------------------------------------
 constexpr int kTile = 64;
 constexpr int kManyLeast = 4;              // tiles per part at least
@@ -594,8 +596,8 @@ constexpr int kReads = 6;
 
 // The row blocks of a ragged batch, longest first: a workgroup that starts late on a long
 // one would end long after the others.  (In which order blocks of one length come is left
-// open; it decides where they run, not what they give.)  5 us; the text rows below take
-// 264 us with it and 328 without.
+// open; it decides where they run, not what they give.)  5 us; the text rows above take
+// 244 us with it and 303 without.
 __global__ __launch_bounds__(kMaxOrder) void attend_order(AttendArgs a, int entries) {
     __shared__ int bin[kMaxOrder], sums[kMaxOrder / 64];
     const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
@@ -1194,7 +1196,9 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 // 17 to 32 are one block of the few-row form where that saves reading codes that no cache holds
 // close (64 x 32 rows over 4096 tokens of 8 heads, 537 MB: 97 us against 180 in two blocks; 16 x
 // 32 over 2048, 67 MB: 27 and 29; 4 x 32 over 4096, 34 MB: 25 and 23.5), not at dp = 256, whose
-// registers hold 16.
+// registers hold 16.  `bytes` goes by the caller's bound of the lengths, which the device alone
+// knows: without one, in tables of 128k tokens, 4 x 32 rows over 4096 take 30.6 us in place of
+// 24.7, 16 x 32 over 2048 33.9 and 26.6.
 static int attend_block_rows(const CacheView& c, long long rows, double bytes) {
     if (rows > 2 * kFewRows) return c.dp == 128 && rows > 128 ? 256 : 128;
     return rows > kFewRows && c.dp <= 128 && bytes >= kFewBytes ? 2 * kFewRows : kFewRows;
@@ -1251,7 +1255,8 @@ AttendShape attend_shape(const CacheView& c, const BatchView& b, int H, long lon
     // The few-row form reads the codes past the caches where nothing reads them twice (one row
     // block per sequence and key head) and they may be more than the last-level cache holds.  64
     // x 4096 tokens of 8 heads take 96 us against 106, with two row blocks each 208 against 177
-    // us; 4 x 2048 tokens 14.7 against 14.3 us.
+    // us; 4 x 2048 tokens 14.7 against 14.3 us.  (At the caller's bound, again: a step over 144 MB
+    // that states 302 takes 63.7 us, and 68.7 where it states less than 256.)
     x.stream = x.few && x.blocks == 1 && bytes > kLastLevelBytes;
     // A call sorts its row blocks, with one more launch, only where rows differ from sequence to
     // sequence and there are blocks for more than a round of the chip, up to a number whose

@@ -8,10 +8,10 @@
 // the order in which threads run.  Freeing subtracts a reference; whoever takes the last
 // one clears the bit.  One workgroup plans a whole call (all or nothing needs one place that
 // knows the total); the per-sequence page lists are walked by a workgroup each.  What
-// bounds these kernels is latency: a handful of dependent loads and barriers.  Room for
-// one sequence's 131 tokens takes 5.2 us, for a token of 32 sequences 6.6 us, for 32 prompts (1300 pages of
-// 64) 11.5 us; forking 32 sequences 4.5 us, freeing them 4.2 us; what 64 pruned forks drop
-// 13.5 us, swapping their pages 4.1 us.
+// bounds these kernels is latency: a handful of dependent loads and barriers.  The kernels
+// themselves: room for one sequence's 131 tokens 5.3 us, for a token of 32 sequences 6.7 us, for
+// 32 prompts (1300 pages of 64) 11.7 us; forking 32 sequences 4.6 us, freeing them 4.1 us; what 64
+// pruned forks drop 13.5 us, swapping their pages 4.0 us.
 #include "cache_internal.hpp"
 
 namespace occam {

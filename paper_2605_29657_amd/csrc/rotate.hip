@@ -14,7 +14,7 @@
 // the pairs (two 16-byte loads and stores where alignment allows), heads and chunks
 // spread over the threads so that consecutive threads touch consecutive addresses.
 // 362 MB of bfloat16 queries and keys: 152 us, 4.8 TB/s in and out (what a large copy
-// reaches); 151 MB of float32, 32 heads of 72: 70 us, 4.3 TB/s; 8 rows: 4.6 us, a launch and
+// reaches); 151 MB of float32, 32 heads of 72: 69 us, 4.4 TB/s; 8 rows: 4.3 us, a launch and
 // three loads.
 #include <string.h>
 
