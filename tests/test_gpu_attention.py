@@ -125,6 +125,18 @@ def test_unequal_scales_over_ranges_and_parts(T, H):
         attend(c, [0], [T], H, scale=1.0, q=q, max_tokens=len(sizes) * 16)
 
 
+@pytest.mark.parametrize("at", range(13))
+@pytest.mark.parametrize("page,H,Hkv,d,T", [(64, 8, 2, 128, 150), (64, 4, 1, 128, 700), (64, 4, 1, 128, 20), (64, 8, 2, 64, 90),
+                                            (64, 2, 1, 256, 90), (64, 4, 2, 128, 2), (64, 24, 1, 64, 1)])
+def test_the_spread_is_passed_at_any_tile(page, H, Hkv, d, T, at):
+    # Ordinary pages up to one of 2^21 (of no weight, or of all rows' largest), and behind it.
+    for z in (-200.0, 0.0):
+        c = unequal(page, H, Hkv, d, [x % 3 for x in range(at)] + [21] + [1] * (12 - at), [0.0] * at + [z] + [0.0] * (12 - at),
+                    seed=at, max_pages=1 << 14)
+        attend(c, [0], [T], H, scale=1.0, q=ones(c, T, H))
+        attend(c, [0], [T], H, scale=1.0, q=ones(c, T, H), max_tokens=13 * page)
+
+
 @pytest.mark.parametrize("T", [1, 5, 16, 150])
 def test_values_next_to_the_largest_float(T):
     # Equal weights of values up to 240 * 2^120: a mean never passes its largest value.
